@@ -420,6 +420,86 @@ int sl_peak_probe_mfma(void *stream, const void *operands, size_t operand_bytes,
                        float *sink, size_t sink_bytes, int64_t *flops);
 int sl_peak_probe_stream(void *stream, const void *src, void *dst, size_t bytes, uint32_t *sink, size_t sink_bytes);
 
+/* ---- few rows with low-bit weights and a low-bit cache ---------------------------------------
+ * The late steps of a run compute few rows, and what they cost is reading: a block's weights and, for long sequences,
+ * the K/V cache.  These calls are the stand-alone low-bit forms of the three pieces involved: the M-row projection with
+ * 4-bit weights, a cache of 8-bit codes in pages, and the rows' attention over it.  They take no context. */
+
+/* 4-bit weights with group scales.  A matrix W [n, k] (out, in) is
+ *   codes  [n, k/2] u8    code of (j, i) in 0..15: the lower (i even) or upper half of byte i/2 of row j
+ *   scales [n, ceil(k/group)] bf16
+ *   zeros  [n, ceil(k/group)] u8, 0..15 (upper halves are ignored); or null: 8 everywhere
+ * and stands for W[j, i] = scales[j, i/group] * (code - zeros[j, i/group]).  group is 32, 64 or 128; n >= 1; k >= 8 and a
+ * multiple of 8 (the last group may be short); n, k <= 2^24.
+ *
+ * sl_linear_q4_quantize: codes, scales and zeros of a plain W (dtype SL_F32 / SL_BF16), nearest code per group, all in fp32:
+ * with zeros, lo = min(0, min w), hi = max(0, max w), scale = bf16((hi - lo) / 15), zero = rint(-lo / scale) in 0..15, code =
+ * rint(w / scale) + zero in 0..15; without, scale = bf16(max|w| / 7), code = rint(w / scale) + 8 in 0..15.  A group of zeros has
+ * scale 0; one that holds a NaN or an infinity has scale NaN, and so has every weight of it.
+ * sl_linear_q4_bytes / sl_linear_q4_pack: size of, and conversion into, the layout sl_linear_q4_forward reads (codes of a
+ * matrix-core operand in one 16-byte load); packed is 16-byte aligned. */
+int sl_linear_q4_quantize(void *stream, const void *w, int32_t dtype, int32_t n, int32_t k, int32_t group, void *codes,
+                          void *scales, void *zeros);
+int sl_linear_q4_bytes(int32_t n, int32_t k, int32_t group, size_t *out);
+int sl_linear_q4_pack(void *stream, const void *codes, const void *scales, const void *zeros, int32_t n, int32_t k,
+                      int32_t group, void *packed, size_t packed_bytes);
+/* y = x W^T for the first min(*m_dev, m_upper) rows of x [m_upper, k] (bf16, row-major, 16-byte aligned), accumulated in fp32;
+ * exactly one of
+ *   y_f32  [m_upper, n] fp32, or
+ *   y_bf16 [*, n] bf16, row r written to row row_map[r] (row_map may be null; only with y_bf16)
+ * is non-null.  Rows past the count are neither read nor written.  No workspace; the same sums in the same order in every
+ * call of one m_upper.  m_upper <= 2^20.  Made for few rows: weights are unpacked once per 64 rows at most, so that hundreds of rows
+ * are a matter of the matrix units; thousands of rows are better served by sl_linear_forward. */
+int sl_linear_q4_forward(void *stream, const void *x, const void *packed, const int32_t *m_dev, int32_t m_upper,
+                         int32_t n, int32_t k, int32_t group, float *y_f32, void *y_bf16, const int32_t *row_map);
+
+/* A K/V cache of one layer in 8 bits, in pages.  Per row and head a vector x of d_head numbers is kept as 8-bit codes and
+ * one fp32 scale: scale = max|x| / 127, code = rint(x / scale) in -127..127, both quotients in fp32; the cached value is
+ * code * scale.  A zero vector has scale 0; a vector that holds a NaN or an infinity reads back as NaN throughout.
+ * A page holds page_slots slots of every head; slot p of sequence b lies in page page_table[b][p / page_slots].  Sequences
+ * take pages as they grow, in any order; a table entry outside 0 .. n_pages - 1 is "no page".  The pool's contents are private
+ * and need no initialisation: what was never written is never part of a result as long as seq_len / row_len leave it out.
+ * The struct is a HOST struct of device pointers, read during the call. */
+typedef struct sl_kv8 {
+  void *pool;                    /* sl_kv8_bytes bytes, 256-byte aligned                                  */
+  size_t pool_bytes;
+  const int32_t *page_table;     /* [batch][max_pages]                                                    */
+  int32_t n_pages;               /* pages of the pool                                                     */
+  int32_t page_slots;            /* 16, 32, 64, 128 or 256                                                */
+  int32_t n_kv_heads, d_head;    /* 1 .. 1024 heads; d_head 32, 64, 128 or 256                            */
+  int32_t batch, max_pages;      /* 1 .. SL_MAX_BATCH sequences; max_pages * page_slots <= 2^30           */
+} sl_kv8;
+int sl_kv8_bytes(int32_t n_pages, int32_t page_slots, int32_t n_kv_heads, int32_t d_head, size_t *out);
+/* Write rows of keys (as attention takes them, after RoPE) and values, or read them back.
+ *   k, v     [m_upper] rows of [n_kv_heads, d_head] (dtype SL_F32 / SL_BF16), k_stride / v_stride elements apart (a
+ *            projection's fused output has such strides); 16-byte aligned, strides a multiple of 16 bytes
+ *   cu_rows  [batch + 1] i32: rows cu_rows[b] .. cu_rows[b + 1] - 1 belong to sequence b (cu_active of a step is one such)
+ *   row_pos  [m_upper] i32: the row's slot in its sequence
+ * Rows from cu_rows[batch] on are left alone.  A row whose slot is negative, past the table or on no page is not written;
+ * read back it is zeros.  Of adjacent rows that name one slot the last is kept; rows that name one slot must be
+ * adjacent.  Values read back are code * scale in fp32, rounded to dtype.  A page may be shared by sequences that read it;
+ * a call must not write one slot through two sequences. */
+int sl_kv8_write(void *stream, const sl_kv8 *kv /* host */, const void *k, const void *v, int32_t dtype, int64_t k_stride,
+                 int64_t v_stride, const int32_t *row_pos, const int32_t *cu_rows, int32_t m_upper);
+int sl_kv8_read(void *stream, const sl_kv8 *kv /* host */, void *k, void *v, int32_t dtype, int64_t k_stride, int64_t v_stride,
+                const int32_t *row_pos, const int32_t *cu_rows, int32_t m_upper);
+/* Attention of each row over the slots of its sequence:
+ *   out[r, h] = sum_p softmax_p(scale * q[r, h] . K[p, h / share]) V[p, h / share],  share = n_heads / n_kv_heads,
+ * p over the first min(seq_len[b], row_len[r]) slots (no more than the table's and than len_upper), without those on no page.
+ * A row that sees no slot gets zeros.
+ *   q, out   [m_upper] rows of [n_heads, d_head] (dtype), q_stride / out_stride elements apart, aligned as above; out must not
+ *            overlap q
+ *   seq_len  [batch] i32;  row_len [m_upper] i32, or null: every row sees its whole sequence
+ *   len_upper      host: an upper bound on the slots any row sees; launches and workspace are sized by it
+ *   workspace      sl_kv8_attention_bytes bytes, 256-byte aligned; needs no initialisation, two calls that may overlap in time
+ *                  must not share one
+ * Rows from cu_rows[batch] on are left as they are.  Scores, softmax statistics and sums are fp32; the same sums in the same
+ * order in every call of the same bounds (no atomics). */
+int sl_kv8_attention_bytes(const sl_kv8 *kv /* host */, int32_t n_heads, int32_t m_upper, int32_t len_upper, size_t *out);
+int sl_kv8_attention(void *stream, const sl_kv8 *kv /* host */, const void *q, int32_t dtype, int64_t q_stride, int32_t n_heads,
+                     const int32_t *cu_rows, const int32_t *seq_len, const int32_t *row_len, int32_t m_upper,
+                     int32_t len_upper, float scale, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes);
+
 /* ---- measurement support ------------------------------------------------------------
  * Per-kernel timing of the step's launches with HIP events on the step's own stream.
  * Between sl_profile_begin and sl_profile_end every kernel the library launches for this

@@ -31,7 +31,13 @@ class sl_weights(C.Structure):
                 ("layers", C.POINTER(sl_layer_weights))]
 
 
-_P, _I, _Z = C.c_void_p, C.c_int32, C.c_size_t
+class sl_kv8(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("pool_bytes", C.c_size_t), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_slots", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("batch", C.c_int32),
+                ("max_pages", C.c_int32)]
+
+
+_P, _I, _Z, _L = C.c_void_p, C.c_int32, C.c_size_t, C.c_int64
 _SIGS = {
     "sl_init": [C.POINTER(sl_config), C.POINTER(_P)],
     "sl_destroy": [_P],
@@ -65,6 +71,15 @@ _SIGS = {
     "sl_linear_plan": [_I, _I, _I, C.POINTER(_I), C.POINTER(_I), C.POINTER(_I), C.POINTER(_I), C.POINTER(_I)],
     "sl_linear_forward": [_P, _P, _I, _P, _P, _I, _I, _I, _I, _P, _P, _P],
     "sl_linear_clock_probe": [_P, _P, _I, _P, _P, _I, _I, _I, _P, _P, _P],
+    "sl_linear_q4_quantize": [_P, _P, _I, _I, _I, _I, _P, _P, _P],
+    "sl_linear_q4_bytes": [_I, _I, _I, C.POINTER(_Z)],
+    "sl_linear_q4_pack": [_P, _P, _P, _P, _I, _I, _I, _P, _Z],
+    "sl_linear_q4_forward": [_P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P],
+    "sl_kv8_bytes": [_I, _I, _I, _I, C.POINTER(_Z)],
+    "sl_kv8_write": [_P, C.POINTER(sl_kv8), _P, _P, _I, _L, _L, _P, _P, _I],
+    "sl_kv8_read": [_P, C.POINTER(sl_kv8), _P, _P, _I, _L, _L, _P, _P, _I],
+    "sl_kv8_attention_bytes": [C.POINTER(sl_kv8), _I, _I, _I, C.POINTER(_Z)],
+    "sl_kv8_attention": [_P, C.POINTER(sl_kv8), _P, _I, _L, _I, _P, _P, _P, _I, _I, C.c_float, _P, _L, _P, _Z],
     "sl_peak_probe_mfma": [_P, _P, _Z, _I, _I, _P, _Z, C.POINTER(C.c_int64)],
     "sl_peak_probe_stream": [_P, _P, _P, _Z, _P, _Z],
     "sl_profile_begin": [_P, _I],
@@ -332,6 +347,90 @@ def sl_linear_clock_probe(x, packed, m_dev, m_upper, n, k, y_bf16, counters, row
 
 def _nbytes(t):
     return t.numel() * t.element_size()
+
+
+# ---- 4-bit weights ---------------------------------------------------------------------------
+def sl_linear_q4_quantize(w, group, codes, scales, zeros=None):
+    """w [n, k]; codes [n, k/2] uint8, scales [n, ceil(k/group)] bfloat16, zeros likewise uint8 or None (see the header)."""
+    n, k = w.shape
+    _check("sl_linear_q4_quantize", lib().sl_linear_q4_quantize(_stream(), _ptr(w), dtype_code(w.dtype), n, k, group, _ptr(codes),
+                                                                _ptr(scales), _ptr(zeros)))
+
+
+def sl_linear_q4_bytes(n, k, group):
+    out = _Z()
+    _check("sl_linear_q4_bytes", lib().sl_linear_q4_bytes(n, k, group, C.byref(out)))
+    return out.value
+
+
+def sl_linear_q4_pack(codes, scales, zeros, n, k, group, packed):
+    _check("sl_linear_q4_pack", lib().sl_linear_q4_pack(_stream(), _ptr(codes), _ptr(scales), _ptr(zeros), n, k, group, _ptr(packed),
+                                                        _nbytes(packed)))
+
+
+def sl_linear_q4_forward(x, packed, m_dev, m_upper, n, k, group, y_f32=None, y_bf16=None, row_map=None):
+    _check("sl_linear_q4_forward", lib().sl_linear_q4_forward(_stream(), _ptr(x), _ptr(packed), _ptr(m_dev), m_upper, n, k, group,
+                                                              _ptr(y_f32), _ptr(y_bf16), _ptr(row_map)))
+
+
+# ---- the paged 8-bit cache -------------------------------------------------------------------
+class KV8:
+    """Owns the pool of a paged 8-bit cache of one layer and holds its page table [batch, max_pages] (int32, device).
+    sequence(b) is the cache seen through one row of the table."""
+
+    def __init__(self, n_pages, page_slots, n_kv_heads, d_head, page_table, pool=None):
+        need = sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head)
+        self.pool = torch.empty(need, dtype=torch.uint8, device=page_table.device) if pool is None else pool
+        self.page_table, self.n_kv_heads, self.d_head = page_table, n_kv_heads, d_head
+        batch, max_pages = page_table.shape
+        self.desc = sl_kv8(_ptr(self.pool), _nbytes(self.pool), _ptr(page_table), n_pages, page_slots, n_kv_heads, d_head, batch,
+                           max_pages)
+
+    def sequence(self, b):
+        return KV8(self.desc.n_pages, self.desc.page_slots, self.n_kv_heads, self.d_head, self.page_table[b:b + 1], self.pool)
+
+
+def sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head):
+    out = _Z()
+    _check("sl_kv8_bytes", lib().sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head, C.byref(out)))
+    return out.value
+
+
+def _head_rows(t, heads, d):
+    """(pointer, row stride in elements) of rows [*, heads, d] that may lie apart; a row itself is dense."""
+    assert t.dim() == 3 and t.shape[1:] == (heads, d) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == d)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _kv8_rows(name, kv, k, v, row_pos, cu_rows, m_upper):
+    assert k.dtype == v.dtype
+    (kp, ks), (vp, vs) = _head_rows(k, kv.n_kv_heads, kv.d_head), _head_rows(v, kv.n_kv_heads, kv.d_head)
+    _check(name, getattr(lib(), name)(_stream(), C.byref(kv.desc), kp, vp, dtype_code(k.dtype), ks, vs, _ptr(row_pos), _ptr(cu_rows),
+                                      m_upper))
+
+
+def sl_kv8_write(kv, k, v, row_pos, cu_rows, m_upper):
+    _kv8_rows("sl_kv8_write", kv, k, v, row_pos, cu_rows, m_upper)
+
+
+def sl_kv8_read(kv, k_out, v_out, row_pos, cu_rows, m_upper):
+    _kv8_rows("sl_kv8_read", kv, k_out, v_out, row_pos, cu_rows, m_upper)
+
+
+def sl_kv8_attention_bytes(kv, n_heads, m_upper, len_upper):
+    out = _Z()
+    _check("sl_kv8_attention_bytes", lib().sl_kv8_attention_bytes(C.byref(kv.desc), n_heads, m_upper, len_upper, C.byref(out)))
+    return out.value
+
+
+def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, workspace, row_len=None):
+    """q, out: rows [*, n_heads, d_head]."""
+    assert q.dtype == out.dtype
+    n_heads = q.shape[1]
+    (qp, qs), (op, os_) = _head_rows(q, n_heads, kv.d_head), _head_rows(out, n_heads, kv.d_head)
+    _check("sl_kv8_attention", lib().sl_kv8_attention(_stream(), C.byref(kv.desc), qp, dtype_code(q.dtype), qs, n_heads, _ptr(cu_rows),
+                                                      _ptr(seq_len), _ptr(row_len), m_upper, len_upper, C.c_float(scale), op, os_,
+                                                      _ptr(workspace), _nbytes(workspace)))
 
 
 def sl_peak_probe_mfma(operands, iters, waves_per_simd, sink):

@@ -1,6 +1,7 @@
 // C-ABI of libsurelock: argument validation, buffer carving and the launch sequence of one
 // SureLock step.  Everything here runs on the host; no device memory is allocated.
 #include "sl_common.h"
+#include "kv8.h"
 #include <new>
 #include <string.h>
 
@@ -698,4 +699,130 @@ extern "C" int sl_unlock_rule(sl_ctx* ctx, void* stream, uint8_t* lock, uint8_t*
   const size_t ts = sl_tsize(ctx->cfg.dtype);
   return slk_posterior_carry(s, ctx->post, ctx->post_buf_elems * ts, (size_t)ctx->cfg.vocab * ts, probe_idx,
                              cu_probe + B, m_upper_probe, t_lock, unlocked, t);
+}
+
+// ---- 4-bit weights -------------------------------------------------------------------------------------
+static bool q4_shape_ok(int32_t n, int32_t k, int32_t group) {
+  return n >= 1 && n <= 1 << 24 && k >= 8 && k <= 1 << 24 && k % 8 == 0 && (group == 32 || group == 64 || group == 128);
+}
+
+extern "C" int sl_linear_q4_quantize(void* stream, const void* w, int32_t dtype, int32_t n, int32_t k, int32_t group, void* codes,
+                                     void* scales, void* zeros) {
+  if (!w || !codes || !scales || !q4_shape_ok(n, k, group)) return SL_EINVAL;
+  if (dtype != SL_F32 && dtype != SL_BF16) return SL_EINVAL;
+  if ((uintptr_t)w % sl_tsize(dtype) || (uintptr_t)scales % 2) return SL_EINVAL;
+  return slk_q4_quantize((hipStream_t)stream, w, dtype, n, k, group, codes, scales, zeros);
+}
+
+extern "C" int sl_linear_q4_bytes(int32_t n, int32_t k, int32_t group, size_t* out) {
+  if (!out || !q4_shape_ok(n, k, group)) return SL_EINVAL;
+  *out = slk_q4_bytes(n, k, group);
+  return SL_OK;
+}
+
+extern "C" int sl_linear_q4_pack(void* stream, const void* codes, const void* scales, const void* zeros, int32_t n, int32_t k,
+                                 int32_t group, void* packed, size_t packed_bytes) {
+  if (!codes || !scales || !packed || !q4_shape_ok(n, k, group)) return SL_EINVAL;
+  if ((uintptr_t)packed % 16 || (uintptr_t)scales % 2) return SL_EINVAL;
+  if (packed_bytes < slk_q4_bytes(n, k, group)) return SL_ENOSPC;
+  return slk_q4_pack((hipStream_t)stream, codes, scales, zeros, n, k, group, packed);
+}
+
+extern "C" int sl_linear_q4_forward(void* stream, const void* x, const void* packed, const int32_t* m_dev, int32_t m_upper, int32_t n,
+                                    int32_t k, int32_t group, float* y_f32, void* y_bf16, const int32_t* row_map) {
+  if (!x || !packed || !m_dev || !q4_shape_ok(n, k, group)) return SL_EINVAL;
+  if (m_upper < 0 || m_upper > 1 << 20 || !y_f32 == !y_bf16 || (row_map && !y_bf16)) return SL_EINVAL;
+  if ((uintptr_t)x % 16 || (uintptr_t)packed % 16 || (uintptr_t)y_f32 % 4 || (uintptr_t)y_bf16 % 2) return SL_EINVAL;
+  if (m_upper == 0) return SL_OK;
+  return slk_q4_linear((hipStream_t)stream, x, packed, m_dev, m_upper, n, k, group, y_f32, y_bf16, row_map);
+}
+
+// ---- the paged 8-bit cache -----------------------------------------------------------------------------
+static bool kv8_shape_ok(int32_t n_pages, int32_t page_slots, int32_t n_kv_heads, int32_t d_head) {
+  if (n_pages < 1 || n_kv_heads < 1 || n_kv_heads > 1024) return false;
+  if (!(page_slots == 16 || page_slots == 32 || page_slots == 64 || page_slots == 128 || page_slots == 256)) return false;
+  return d_head == 32 || d_head == 64 || d_head == 128 || d_head == 256;
+}
+
+extern "C" int sl_kv8_bytes(int32_t n_pages, int32_t page_slots, int32_t n_kv_heads, int32_t d_head, size_t* out) {
+  if (!out || !kv8_shape_ok(n_pages, page_slots, n_kv_heads, d_head)) return SL_EINVAL;
+  *out = (size_t)n_pages * n_kv_heads * (page_slots / 16) * (32 * (size_t)d_head + 128);
+  return SL_OK;
+}
+
+static int kv8_check(const sl_kv8* kv) {
+  if (!kv || !kv->pool || !kv->page_table || (uintptr_t)kv->pool % 256 || (uintptr_t)kv->page_table % 4) return SL_EINVAL;
+  size_t need = 0;
+  SL_TRY(sl_kv8_bytes(kv->n_pages, kv->page_slots, kv->n_kv_heads, kv->d_head, &need));
+  if (kv->batch < 1 || kv->batch > SL_MAX_BATCH || kv->max_pages < 1) return SL_EINVAL;
+  if ((int64_t)kv->max_pages * kv->page_slots > (int64_t)1 << 30) return SL_EINVAL;
+  return kv->pool_bytes < need ? SL_ENOSPC : SL_OK;
+}
+
+static Kv8View kv8_view(const sl_kv8* kv) {
+  Kv8View v;
+  v.pool = (unsigned char*)kv->pool;
+  v.table = kv->page_table;
+  v.n_pages = kv->n_pages;
+  v.page_shift = __builtin_ctz((unsigned)kv->page_slots);
+  v.heads = kv->n_kv_heads;
+  v.batch = kv->batch;
+  v.max_pages = kv->max_pages;
+  return v;
+}
+
+// rows of `width` numbers, `stride` apart, that the kernels read in 16-byte pieces
+static bool kv8_rows_ok(const void* p, int64_t stride, int64_t width, int32_t dtype) {
+  return p && (uintptr_t)p % 16 == 0 && stride >= width && stride <= (int64_t)1 << 40 && stride * (int64_t)sl_tsize(dtype) % 16 == 0;
+}
+
+static int kv8_check_rows(const sl_kv8* kv, const void* k, const void* v, int32_t dtype, int64_t k_stride, int64_t v_stride,
+                          const int32_t* row_pos, const int32_t* cu_rows, int32_t m_upper) {
+  SL_TRY(kv8_check(kv));
+  if (!row_pos || !cu_rows || m_upper < 0 || (dtype != SL_F32 && dtype != SL_BF16)) return SL_EINVAL;
+  const int64_t width = (int64_t)kv->n_kv_heads * kv->d_head;
+  return kv8_rows_ok(k, k_stride, width, dtype) && kv8_rows_ok(v, v_stride, width, dtype) ? SL_OK : SL_EINVAL;
+}
+
+extern "C" int sl_kv8_write(void* stream, const sl_kv8* kv, const void* k, const void* v, int32_t dtype, int64_t k_stride,
+                            int64_t v_stride, const int32_t* row_pos, const int32_t* cu_rows, int32_t m_upper) {
+  SL_TRY(kv8_check_rows(kv, k, v, dtype, k_stride, v_stride, row_pos, cu_rows, m_upper));
+  if (m_upper == 0) return SL_OK;
+  return slk_kv8_write((hipStream_t)stream, kv8_view(kv), kv->d_head, dtype, k, v, k_stride, v_stride, row_pos, cu_rows, m_upper);
+}
+
+extern "C" int sl_kv8_read(void* stream, const sl_kv8* kv, void* k, void* v, int32_t dtype, int64_t k_stride, int64_t v_stride,
+                           const int32_t* row_pos, const int32_t* cu_rows, int32_t m_upper) {
+  SL_TRY(kv8_check_rows(kv, k, v, dtype, k_stride, v_stride, row_pos, cu_rows, m_upper));
+  if (m_upper == 0) return SL_OK;
+  return slk_kv8_read((hipStream_t)stream, kv8_view(kv), kv->d_head, dtype, k, v, k_stride, v_stride, row_pos, cu_rows, m_upper);
+}
+
+static int kv8_attention_shape(const sl_kv8* kv, int32_t n_heads, int32_t m_upper, int32_t len_upper) {
+  SL_TRY(kv8_check(kv));
+  if (n_heads < 1 || n_heads > 1 << 16 || n_heads % kv->n_kv_heads || m_upper < 0 || m_upper > 1 << 20 || len_upper < 0) return SL_EINVAL;
+  if ((int64_t)m_upper * n_heads > (int64_t)1 << 28) return SL_EINVAL;
+  return SL_OK;
+}
+
+extern "C" int sl_kv8_attention_bytes(const sl_kv8* kv, int32_t n_heads, int32_t m_upper, int32_t len_upper, size_t* out) {
+  if (!out) return SL_EINVAL;
+  SL_TRY(kv8_attention_shape(kv, n_heads, m_upper, len_upper));
+  *out = slk_kv8_attention_bytes(kv8_view(kv), kv->d_head, n_heads, m_upper, len_upper);
+  return SL_OK;
+}
+
+extern "C" int sl_kv8_attention(void* stream, const sl_kv8* kv, const void* q, int32_t dtype, int64_t q_stride, int32_t n_heads,
+                                const int32_t* cu_rows, const int32_t* seq_len, const int32_t* row_len, int32_t m_upper,
+                                int32_t len_upper, float scale, void* out, int64_t out_stride, void* workspace, size_t workspace_bytes) {
+  SL_TRY(kv8_attention_shape(kv, n_heads, m_upper, len_upper));
+  if (!cu_rows || !seq_len || !workspace || (uintptr_t)workspace % 256 || (dtype != SL_F32 && dtype != SL_BF16)) return SL_EINVAL;
+  const int64_t width = (int64_t)n_heads * kv->d_head;
+  if (!kv8_rows_ok(q, q_stride, width, dtype) || !kv8_rows_ok(out, out_stride, width, dtype)) return SL_EINVAL;
+  if (!(scale > 0.f) || !(scale < __builtin_inff())) return SL_EINVAL;
+  if (m_upper == 0) return SL_OK;
+  const Kv8View v = kv8_view(kv);
+  if (workspace_bytes < slk_kv8_attention_bytes(v, kv->d_head, n_heads, m_upper, len_upper)) return SL_ENOSPC;
+  return slk_kv8_attention((hipStream_t)stream, v, kv->d_head, dtype, q, q_stride, n_heads, cu_rows, seq_len, row_len, m_upper, len_upper,
+                           scale, out, out_stride, workspace);
 }

@@ -366,6 +366,12 @@ int slk_wavek_swiglu_ok(int mu, int dff, int k);
 int slk_wavek_swiglu(hipStream_t s, const void* A, const void* Wp, const int32_t* m_dev, int mu, int dff, int k, void* a);
 int slk_wavek_splits(int mu, int n, int k);
 int slk_wavek_planes(hipStream_t s, const void* A, const void* Wp, const int32_t* m_dev, int mu, int n, int k, float* Cf);
+// gemm_q4.hip: products with 4-bit weights
+size_t slk_q4_bytes(int n, int k, int group);
+int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int group, void* codes, void* scales, void* zeros);
+int slk_q4_pack(hipStream_t s, const void* codes, const void* scales, const void* zeros, int n, int k, int group, void* packed);
+int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
+                  void* y_bf16, const int32_t* row_map);
 // attention_mfma.hip
 int slk_attention_mfma(hipStream_t s, const void* q, const void* kc, const void* vc, const int32_t* active_idx,
                        const int32_t* m_dev, int m_upper, int B, int H, int N, int n_pad, void* o, float* scratch);
