@@ -4,11 +4,12 @@
 // rint(x / scale), value = code * scale.  16 slots of one head are a tile,
 //   [K codes 16 d][V codes 16 d][16 K scales][16 V scales]
 // and a page holds page_slots / 16 tiles of every head, a head's tiles behind one another.  Inside a tile the codes lie in the
-// order in which the matrix cores take them (16x16x32 products, lane l: row l % 16, reduction indexes 8 (l / 16) .. + 7), so a
+// order in which the matrix cores take them (16-row products, lane l: row l % 16, the (l / 16)-th quarter of the reduction), so a
 // lane's share of an operand is one load of 16 bytes (8 with d = 32) and a wave's load is one contiguous KiB:
-//   K  [d / 4E][4][16 slots][E dims]            E = 16 (8 with d = 32): two products' worth of reduction indexes a lane
-//   V  [d / 4E][4][16 dims][E / 4][4 slots]     reduction over slots: the scores' product K Q^T leaves slots 4 (l / 16) .. + 3 of
-//                                               a tile in lane l, so probabilities become the second product's operand in place
+//   K  [d / 4E][4][16 slots][E dims]            signed bytes, E = 16 (8 with d = 32): the operand of a product of 8-bit integers
+//   V  [d / 4E][4][16 dims][E / 4][4 slots]     code + 128; reduction over slots: the scores' product K Q^T leaves slots
+//                                               4 (l / 16) .. + 3 of a tile in lane l, so probabilities become the second
+//                                               product's operand in place
 #pragma once
 #include "sl_common.h"
 

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(Kv8View kv, const T* k, 
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
       tile[Tile::k_at(slot, lane * NP + e)] = (unsigned char)(signed char)(int)kc[e];
-      tile[Tile::v_at(slot, lane * NP + e)] = (unsigned char)(signed char)(int)vc[e];
+      tile[Tile::v_at(slot, lane * NP + e)] = (unsigned char)((int)vc[e] + 128);
     }
   }
   if (lane == 0) {
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void kv8_read_kernel(Kv8View kv, T* k, T* v, i
   for (int e = 0; e < NP; ++e) {
     const int dim = lane * NP + e;
     const float kq = ok ? (float)(signed char)tile[Tile::k_at(slot, dim)] : 0.f;
-    const float vq = ok ? (float)(signed char)tile[Tile::v_at(slot, dim)] : 0.f;
+    const float vq = ok ? (float)((int)tile[Tile::v_at(slot, dim)] - 128) : 0.f;
     st<T>::stv(k + (size_t)r * k_stride + head * D + dim, kq * ks);
     st<T>::stv(v + (size_t)r * v_stride + head * D + dim, vq * vs);
   }
