@@ -800,7 +800,7 @@ extern "C" int sl_kv8_read(void* stream, const sl_kv8* kv, void* k, void* v, int
 
 static int kv8_attention_shape(const sl_kv8* kv, int32_t n_heads, int32_t m_upper, int32_t len_upper) {
   SL_TRY(kv8_check(kv));
-  if (n_heads < 1 || n_heads > 1 << 16 || n_heads % kv->n_kv_heads || m_upper < 0 || m_upper > 1 << 20 || len_upper < 0) return SL_EINVAL;
+  if (n_heads < 1 || n_heads > 1 << 14 || n_heads % kv->n_kv_heads || m_upper < 0 || m_upper > 1 << 20 || len_upper < 0) return SL_EINVAL;
   if ((int64_t)m_upper * n_heads > (int64_t)1 << 28) return SL_EINVAL;
   return SL_OK;
 }

@@ -7,7 +7,7 @@
 // and slots 4 (l / 16) .. + 3 of a tile, which is the operand the second product wants, so probabilities never leave registers.
 //
 // Unpacking codes is what such a kernel would spend its time on: an integer-to-float conversion costs a wave four times an
-// addition, and as bf16 by conversion K and V took 14 us per step of 64 slots and wave where three waves shared a SIMD.  So
+// addition, and with K and V converted to bf16 the largest case took 291 us, 180 as follows (memory alone 170 at that stage):
 //   K is not unpacked: the product is one of 8-bit integers, the query being a fixed-point number of three signed bytes,
 //     q = 2^(e - 22) (65536 a + 256 b + c), 2^(e-1) <= max|q| < 2^e: 23 bits of the row's largest number, as good as fp32's own sums.
 //     Each byte's product starts from the integer 0x4B400000, whose bits are the float 1.5 * 2^23, so that the result, below 2^22
@@ -44,8 +44,29 @@ template <> struct Piece<16> {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
+// (loads of codes that no other workgroup asks for go past the caches' replacement: 830 MB in 133 us instead of 153)
+template <bool ONCE, typename P>
+__device__ inline P ask(const P* p) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(P) / 4)));
+  if constexpr (!ONCE) return *p;
+  const words w = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+  P r;
+  __builtin_memcpy(&r, &w, sizeof(P));
+  return r;
+}
 template <typename P>
 __device__ inline uint32_t word(const P& p, int i) { return reinterpret_cast<const uint32_t*>(&p)[i]; }
+
+// the other lanes' value, 16 / 32 lanes away, taken into a maximum or a sum without going through LDS
+template <typename F>
+__device__ inline float across_groups(float x, F f) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float max_across(float x) { return across_groups(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ inline float sum_across(float x) { return across_groups(x, [](float a, float b) { return a + b; }); }
 
 // V's codes (each + 128) of 4 slots of one tile and 4 of the next, as halves
 __device__ inline f16x8 v_halves(uint32_t a, uint32_t b) {
@@ -57,131 +78,182 @@ __device__ inline f16x8 v_halves(uint32_t a, uint32_t b) {
   return f16x8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
 }
 
-// x = 2^-22 times three signed bytes in base 256, for x of at most 2^22 in magnitude
-__device__ inline void three_bytes(float x, int& a, int& b, int& c) {
-  const int i = (int)rintf(x);
-  c = (int)(signed char)i;
-  const int j = (i - c) >> 8;
-  b = (int)(signed char)j;
-  a = (j - b) >> 8;
+// Four numbers of at most 2^22 in magnitude as three signed bytes each, base 256: byte p of all four in w[p].  A number plus
+// 0x808080 has unsigned bytes, each 128 more than the signed ones; flipping their top bits takes the 128 off again.
+__device__ inline void signed_bytes(const float (&x)[4], uint32_t (&w)[3]) {
+  uint32_t j[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) j[i] = ((uint32_t)(int)rintf(x[i]) + 0x808080u) ^ 0x808080u;
+  const uint32_t low01 = __builtin_amdgcn_perm(j[1], j[0], 0x05040100u), low23 = __builtin_amdgcn_perm(j[3], j[2], 0x05040100u);
+  const uint32_t high = __builtin_amdgcn_perm(j[1], j[0], 0x0c0c0602u);
+  w[0] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(j[3], j[2], 0x0c0c0602u), high, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(low23, low01, 0x07050301u);
+  w[2] = __builtin_amdgcn_perm(low23, low01, 0x06040200u);
 }
 
+constexpr int kResident = 3;                              // workgroups of a CU that registers let run at once (2 with d = 256)
+// Pieces wanted, in rounds of what runs at once.  us at 1, 2, 3, 4, 6 rounds: one row in each of 8 ragged sequences 59, 52, 55, 56, 61;
+// 16 long ragged ones 162, 156, 149, 153, 160; one longer round ends when its last workgroup does, many short ones start often.
+constexpr int kRounds = 2;
+// Units of a piece, at least (us at 1, 2, 4: 64 rows of 2048 slots 25.7, 25.9, 22.5; one row of 4096 slots 18.5, 16.6, 17.4): up to
+// 512 slots a segment is one piece and the second launch falls away.
+constexpr int kLeast = 4;
+
+// A segment is a tile of queries with one K/V head: sequence by sequence, head by head, tile by tile.  Segments are cut into pieces of
+// nearly equal length, one for each workgroup, so long that there are about a.pieces of them however ragged the lengths are
+// (every workgroup works that out from the row counts and lengths).  Of a segment in several pieces each leaves a partial result,
+// and a second launch joins those.
 struct Kv8Attn {
   const void* q;
   void* out;
-  float* part;                                            // partial results of the chunks, or null: one chunk
+  float* part;                                            // partial results
   const int32_t *cu_rows, *seq_len, *row_len;
   int64_t q_stride, out_stride;
   int n_heads, share, m_upper, len_upper;                 // share = query heads per K/V head
-  int chunk, chunks;                                      // slots a workgroup takes, and how many such there are
+  int unit, pieces;                                       // slots a length is counted in; pieces wanted
   float scale_log2;                                       // scale * log2(e): probabilities are powers of two
-  __device__ int rows_of(int b, int& row0) const {
-    row0 = min(max(cu_rows[b], 0), m_upper);
-    return min(max(cu_rows[b + 1] - row0, 0), m_upper - row0);
-  }
-  __device__ int limit_of(int b, int r, int slots) const {
-    int n = min(min(max(seq_len[b], 0), slots), len_upper);
-    if (row_len) n = min(n, row_len[r]);
-    return n;
-  }
-  // partial sums [row and head][chunk][d], behind them maximum and sum [row and head][chunk]
-  __device__ float* sums(size_t rh, int c, int d) const { return part + (rh * chunks + c) * d; }
-  __device__ float2* stats(size_t rh, int c, int d) const {
-    return reinterpret_cast<float2*>(part + (size_t)m_upper * n_heads * chunks * d) + rh * chunks + c;
-  }
+  // partial p: sums [16 queries][d]; behind all of them maximum and sum.  Fewer than 2 pieces: a segment of n units in k > 1
+  // pieces has k < n / c + 1 < 2 n / c, where all n together are at most c pieces
+  __device__ float* sums(int p, int col, int d) const { return part + ((size_t)p * 16 + col) * d; }
+  __device__ float2* stats(int p, int col, int d) const { return reinterpret_cast<float2*>(part + (size_t)pieces * 32 * d) + (size_t)p * 16 + col; }
 };
 
-// Tile `t` of `width` queries -> its sequence, its first query there, the sequence's rows; false past the last tile.  A wave
-// asks together: 64 sequences' tiles at once, added up along the lanes.
-__device__ inline bool kv8_tile_of(const Kv8Attn& a, int batch, int width, int t, int& b, int& first, int& row0, int& rows) {
-  const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < batch; b0 += 64) {
-    int start = 0, n = 0;
-    if (b0 + lane < batch) n = a.rows_of(b0 + lane, start);
-    const int tiles = (n * a.share + width - 1) / width;
-    int upto = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int before = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += before;
-    }
-    const uint64_t past = __ballot(upto > t);
-    if (past) {
-      const int at = __builtin_ffsll((long long)past) - 1;
-      b = __builtin_amdgcn_readfirstlane(b0 + at);
-      first = __builtin_amdgcn_readfirstlane((t - __shfl(upto - tiles, at, 64)) * width);
-      row0 = __builtin_amdgcn_readfirstlane(__shfl(start, at, 64));
-      rows = __builtin_amdgcn_readfirstlane(__shfl(n, at, 64));
-      return true;
-    }
-    t -= __shfl(upto, 63, 64);
-  }
-  return false;
+struct Kv8Sequence { int row0, rows, len, tiles, units; };      // tiles of its queries, units of its length (one at least)
+
+__device__ inline Kv8Sequence kv8_sequence(const Kv8View& kv, const Kv8Attn& a, int b) {
+  Kv8Sequence s;
+  s.row0 = min(max(a.cu_rows[b], 0), a.m_upper);
+  s.rows = min(max(a.cu_rows[b + 1] - s.row0, 0), a.m_upper - s.row0);
+  s.len = min(min(max(a.seq_len[b], 0), kv.slots()), a.len_upper);
+  s.tiles = (s.rows * a.share + 15) / 16;
+  s.units = max((s.len + a.unit - 1) / a.unit, 1);
+  return s;
 }
 
-constexpr int kWaves = 4, kStepTiles = 4;                 // a wave takes 64 slots a step
-constexpr int kStep = 16 * kStepTiles;
-
-// One workgroup: one K/V head, QT tiles of 16 queries, one chunk of the slots; its waves take the steps in turn.
-template <typename T, int D, int QT>
-__global__ __launch_bounds__(64 * kWaves) void kv8_attention_kernel(Kv8View kv, Kv8Attn a) {
-  using Tile = Kv8Tile<D>;
-  constexpr int E = Tile::E, CH = Tile::CH, DT = D / 16;
-  typedef typename Piece<E>::type piece;
-  __shared__ float o_sh[kWaves][16][D + 4];
-  __shared__ float m_sh[kWaves][16 * QT], l_sh[kWaves][16 * QT];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
-  const int kvh = blockIdx.y, chunk0 = blockIdx.z * a.chunk;
-  int b, first, row0, rows;
-  if (!kv8_tile_of(a, kv.batch, 16 * QT, blockIdx.x, b, first, row0, rows)) return;
-  const int queries = rows * a.share;
-  int limit[QT], most = 0, least = 1 << 30;               // of the tile's queries
-  piece qd[QT][CH][3];                                    // the query's bytes
-  int qe[QT];                                             // its exponent - 22
-  float qnan[QT];                                         // NaN for a query that is not finite, else 0
+__device__ inline int wave_sum_int(int x) {
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int f = first + 16 * t + col;
-    const bool live = f < queries;
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// Units of a piece, at most, from all segments' units; a wave asks for 64 sequences at a time and keeps the first 64.
+__device__ inline int kv8_piece(const Kv8View& kv, const Kv8Attn& a, Kv8Sequence& mine) {
+  const int lane = threadIdx.x & 63;
+  int all = 0;
+  for (int b = lane; b < kv.batch; b += 64) {
+    const Kv8Sequence s = kv8_sequence(kv, a, b);
+    if (b == lane) mine = s;
+    all += s.tiles * kv.heads * s.units;
+  }
+  all = wave_sum_int(all);
+  return max((all + a.pieces - 1) / a.pieces, kLeast);
+}
+
+constexpr int kWaves = 4, ST = 2, kStep = 16 * ST;        // a wave takes 32 slots a step
+constexpr int kUnit = kWaves * kStep, kPages = 64 / ST;
+
+// slots [from, end) of one segment: K/V head `kvh`, the 16 queries from `first` on of sequence b
+template <typename T, int D, bool ONCE>
+struct Kv8Segment {
+  using Tile = Kv8Tile<D>;
+  static constexpr int E = Tile::E, CH = Tile::CH, DT = D / 16;
+  typedef typename Piece<E>::type piece;
+  struct Shared {
+    float o[kWaves][16][D + 4];
+    float m[kWaves][16], l[kWaves][16];
+    __attribute__((aligned(16))) uint32_t q[CH][3][64][E / 4];       // the queries' bytes
+  };
+  static __device__ __forceinline__ void run(const Kv8View& kv, const Kv8Attn& a, Shared& sh, int b, const Kv8Sequence& seq, int kvh, int first,
+                                             int from, int end, int part);
+};
+
+template <typename T, int D, bool ONCE>
+__device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, const Kv8Attn& a, Shared& sh, int b, const Kv8Sequence& seq, int kvh,
+                                                            int first, int from, int end, int part) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  const int queries = seq.rows * a.share, row0 = seq.row0, len = seq.len;
+  // the codes of a step: K's are asked for one step ahead once the scores are done, V's once the sums are
+  int pages = 0;                                          // lane i: the page of tile i % ST of the (i / ST)-th of kPages steps
+  auto ask_pages = [&](int s0) {
+    const int slot = s0 + (lane / ST) * (kWaves * kStep) + lane % ST * 16;
+    pages = slot < end ? kv.table[(size_t)b * kv.max_pages + (slot >> kv.page_shift)] : -1;
+  };
+  const unsigned char* tile[ST];
+  int ok = 0;                                             // bit j: tile j is on a page
+  piece kc[ST][CH], vc[ST][CH];
+  f32x4 ks[ST], vs[ST];
+  auto ask_k = [&](int s0, int step) {
+    ok = 0;
+#pragma unroll
+    for (int j = 0; j < ST; ++j) {
+      const int page = __builtin_amdgcn_readlane(pages, step % kPages * ST + j);
+      const bool there = page >= 0 && page < kv.n_pages;
+      ok |= there << j;
+      tile[j] = kv.tile<D>(there ? page : 0, kvh, s0 + 16 * j);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) kc[j][c] = ask<ONCE>(reinterpret_cast<const piece*>(tile[j]) + c * 64 + lane);
+      ks[j] = *reinterpret_cast<const f32x4*>(tile[j] + Tile::kKs + 16 * grp);
+    }
+  };
+  auto ask_v = [&]() {
+#pragma unroll
+    for (int j = 0; j < ST; ++j) {
+      vs[j] = *reinterpret_cast<const f32x4*>(tile[j] + Tile::kVs + 16 * grp);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) vc[j][c] = ask<ONCE>(reinterpret_cast<const piece*>(tile[j] + Tile::kV) + c * 64 + lane);
+    }
+  };
+  int s0 = from + wave * kStep;
+  ask_pages(s0);
+
+  const int f = first + col;
+  const bool live = f < queries;
+  constexpr int QW = E * sizeof(T) / 16;                  // 16-byte words of this lane's share of a chunk
+  uint4 x[CH][QW];
+  int limit = 0;
+  {
     const int r = row0 + (live ? f / a.share : 0), h = kvh * a.share + (live ? f % a.share : 0);
-    limit[t] = live ? a.limit_of(b, r, kv.slots()) : 0;
-    most = max(most, limit[t]);
-    if (live) least = min(least, limit[t]);
+    if (live) limit = a.row_len ? min(len, a.row_len[r]) : len;
     const T* qr = (const T*)a.q + (size_t)r * a.q_stride + (size_t)h * D;
-    float x[CH][E];
-    uint32_t big = 0;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int u = 0; u < E; u += 8) {
-        float y[8];
-        if constexpr (sizeof(T) == 2) ld8(qr + c * 4 * E + grp * E + u, y); else ld8f(qr + c * 4 * E + grp * E + u, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[c][u + e] = y[e];
-          big = max(big, __float_as_uint(y[e]) & 0x7fffffffu);
-        }
-      }
-    big = max(big, (uint32_t)__shfl_xor((int)big, 16, 64));
-    big = max(big, (uint32_t)__shfl_xor((int)big, 32, 64));
-    const bool finite = big < 0x7f800000u;
-    const int e = finite ? __builtin_amdgcn_frexp_expf(__uint_as_float(big)) : 0;
-    qe[t] = e - 22;
-    qnan[t] = finite ? 0.f : __builtin_nanf("");
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      uint32_t w[3][E / 4] = {};
-#pragma unroll
-      for (int u = 0; u < E; ++u) {
-        int d[3];
-        three_bytes(finite ? __builtin_amdgcn_ldexpf(x[c][u], 22 - e) : 0.f, d[0], d[1], d[2]);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][u / 4] |= (uint32_t)(d[p] & 255) << (u % 4 * 8);
-      }
-#pragma unroll
-      for (int p = 0; p < 3; ++p) __builtin_memcpy(&qd[t][c][p], w[p], E);
-    }
+      for (int u = 0; u < QW; ++u) x[c][u] = reinterpret_cast<const uint4*>(qr + c * 4 * E + grp * E)[u];
   }
+  auto x_at = [&](int c, int u) {                         // number u of chunk c
+    if constexpr (sizeof(T) == 2) return __uint_as_float(u % 2 ? word(x[c][u / 8], u / 2 % 4) & 0xffff0000u : word(x[c][u / 8], u / 2 % 4) << 16);
+    else return __uint_as_float(word(x[c][u / 4], u % 4));
+  };
+  ask_k(s0, 0);                                           // (a wave without a step of its own asks for page 0: no branch)
+  ask_v();
+  // every wave knows its queries' exponents; the bytes are shared out among the waves
+  uint32_t big = 0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int u = 0; u < E; ++u) big = max(big, __float_as_uint(x_at(c, u)) & 0x7fffffffu);
+  big = __float_as_uint(across_groups(__uint_as_float(big), [](float p, float q) {
+    return __uint_as_float(max(__float_as_uint(p), __float_as_uint(q)));
+  }));
+  const bool finite = big < 0x7f800000u;
+  const int qe = finite ? __builtin_amdgcn_frexp_expf(__uint_as_float(big)) : 0;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int u = 0; u < E; u += 4)
+      if ((c * E + u) / 4 % kWaves == wave) {
+        float y[4];
+        uint32_t w[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_ldexpf(x_at(c, u + i), 22 - qe);
+        signed_bytes(y, w);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) sh.q[c][p][lane][u / 4] = w[p];
+      }
+  // scores come out in powers of two: 2^(qe - 22), scale and log2(e) in one factor; NaN for a query that is not finite
+  const float unit = finite ? __builtin_amdgcn_ldexpf(a.scale_log2, qe - 22) : __builtin_nanf("");
+  const float unit_a = unit * 65536.f, unit_b = unit * 256.f, unit_c = -kMagic * unit;
+  int most = limit, least = live ? limit : 1 << 30;
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
     most = max(most, __shfl_xor(most, o, 64));
@@ -189,225 +261,257 @@ __global__ __launch_bounds__(64 * kWaves) void kv8_attention_kernel(Kv8View kv, 
   }
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
-  if (a.part && chunk0 >= most) return;                   // the join does not ask for it
-  const int end = min(most, chunk0 + a.chunk);
+  end = min(most, end);
+  __syncthreads();
 
-  f32x4 o[QT][DT] = {};
-  float m[QT], l[QT];                                     // of this wave's slots; l of this lane's
-  int top[QT];                                            // o is scaled by 2^(kTop - top)
+  f32x4 o[DT] = {};
+  float m = kNegInf, l = 0.f;                             // of this wave's slots; l of this lane's
+  int top = -300;                                         // o is scaled by 2^(kTop - top)
+  for (int step = 0; s0 < end; ++step) {
+    const int here = s0, ok_here = ok;
+    const bool whole = here + kStep <= least && ok == (1 << ST) - 1;      // every query sees every slot of the step
+    s0 += kWaves * kStep;
+    float s[ST][4];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) { m[t] = kNegInf; l[t] = 0.f; top[t] = -300; }
-  int pages = 0;                                          // lane i: the page of tile i % 4 of the (i / 4)-th of 16 steps
-  for (int s0 = chunk0 + wave * kStep, step = 0; s0 < end; s0 += kWaves * kStep, ++step) {
-    if (step % 16 == 0) {
-      const int slot = s0 + (lane / kStepTiles) * (kWaves * kStep) + lane % kStepTiles * 16;
-      pages = slot < end ? kv.table[(size_t)b * kv.max_pages + (slot >> kv.page_shift)] : -1;
-    }
-    const unsigned char* tile[kStepTiles];
-    bool ok[kStepTiles], whole = s0 + kStep <= least;     // whole: every query sees every slot of the step
-#pragma unroll
-    for (int j = 0; j < kStepTiles; ++j) {
-      const int page = __builtin_amdgcn_readlane(pages, step % 16 * kStepTiles + j);
-      ok[j] = page >= 0 && page < kv.n_pages;
-      whole &= ok[j];
-      tile[j] = kv.tile<D>(ok[j] ? page : 0, kvh, s0 + 16 * j);
-    }
-    piece kc[kStepTiles][CH], vc[kStepTiles][CH];
-    f32x4 ks[kStepTiles], vs[kStepTiles];
-#pragma unroll
-    for (int j = 0; j < kStepTiles; ++j) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) kc[j][c] = reinterpret_cast<const piece*>(tile[j])[c * 64 + lane];
-      ks[j] = *reinterpret_cast<const f32x4*>(tile[j] + Tile::kKs + 16 * grp);
-    }
-#pragma unroll
-    for (int j = 0; j < kStepTiles; ++j) {
-      vs[j] = *reinterpret_cast<const f32x4*>(tile[j] + Tile::kVs + 16 * grp);
-#pragma unroll
-      for (int c = 0; c < CH; ++c) vc[j][c] = reinterpret_cast<const piece*>(tile[j] + Tile::kV)[c * 64 + lane];
-    }
-    float s[QT][kStepTiles][4];
-#pragma unroll
-    for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        const i32x4 zero = {kMagicBits, kMagicBits, kMagicBits, kMagicBits};
-        i32x4 acc[3] = {zero, zero, zero};
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int p = 0; p < 3; ++p) acc[p] = Piece<E>::mfma(kc[j][c], qd[t][c][p], acc[p]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = fmaf(__int_as_float(acc[0][i]) - kMagic, 65536.f,
-                               fmaf(__int_as_float(acc[1][i]) - kMagic, 256.f, __int_as_float(acc[2][i]) - kMagic));
-          s[t][j][i] = __builtin_amdgcn_ldexpf(fmaf(x, ks[j][i] * a.scale_log2, qnan[t]), qe[t]);
-        }
-      }
-    if (!whole) {
-#pragma unroll
-      for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int slot = s0 + 16 * j + 4 * grp + i;
-#pragma unroll
-          for (int t = 0; t < QT; ++t)
-            if (!ok[j] || slot >= limit[t]) s[t][j][i] = kNegInf;
-        }
-    }
-    f16x8 hi[QT][kStepTiles / 2], lo[QT][kStepTiles / 2];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float best = kNegInf, w[kStepTiles][4], most_w = 0.f;
-#pragma unroll
-      for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) best = fmaxf(best, s[t][j][i]);
-      best = fmaxf(best, __shfl_xor(best, 16, 64));
-      best = fmaxf(best, __shfl_xor(best, 32, 64));
-      const float m_new = fmaxf(m[t], best), base = m_new == kNegInf ? 0.f : m_new;
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = s[t][j][i], p = __builtin_amdgcn_exp2f(x - base);
-          sum += p;
-          w[j][i] = x == kNegInf ? 0.f : p * vs[j][i];    // (the scale of a slot that this query does not see may be NaN)
-          most_w = fmaxf(most_w, w[j][i]);
-        }
-      most_w = fmaxf(most_w, __shfl_xor(most_w, 16, 64));
-      most_w = fmaxf(most_w, __shfl_xor(most_w, 32, 64));
-      const int top_new = max(top[t], most_w > 0.f ? __builtin_amdgcn_frexp_expf(most_w) : -300);
-      const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
-      l[t] = fmaf(l[t], alpha, sum);
-      if (__any(top_new != top[t] || m_new != m[t])) {
-        const float beta = __builtin_amdgcn_ldexpf(alpha, top[t] - top_new);
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[t][i] *= beta;
-      }
-      m[t] = m_new;
-      top[t] = top_new;
-#pragma unroll
-      for (int j = 0; j < kStepTiles; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = __builtin_amdgcn_ldexpf(w[j][i], kTop - top_new);
-          const _Float16 h = (_Float16)x;
-          hi[t][j / 2][j % 2 * 4 + i] = h;
-          lo[t][j / 2][j % 2 * 4 + i] = (_Float16)(x - (float)h);
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kStepTiles; j += 2)
+    for (int j = 0; j < ST; ++j) {
+      const i32x4 zero = {kMagicBits, kMagicBits, kMagicBits, kMagicBits};
+      i32x4 acc[3] = {zero, zero, zero};
 #pragma unroll
       for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int u = 0; u < E / 4; ++u) {
-          const f16x8 vf = v_halves(word(vc[j][c], u), word(vc[j + 1][c], u));
+        for (int p = 0; p < 3; ++p) acc[p] = Piece<E>::mfma(kc[j][c], *reinterpret_cast<const piece*>(sh.q[c][p][lane]), acc[p]);
 #pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            f32x4& acc = o[t][c * (E / 4) + u];
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[t][j / 2], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[t][j / 2], acc, 0, 0, 0);
+      for (int i = 0; i < 4; ++i)
+        s[j][i] = ks[j][i] * fmaf(__int_as_float(acc[0][i]) - kMagic, unit_a,
+                                  fmaf(__int_as_float(acc[1][i]) - kMagic, unit_b, fmaf(__int_as_float(acc[2][i]), unit, unit_c)));
+    }
+    if (s0 < end) {
+      if ((step + 1) % kPages == 0) ask_pages(s0);
+      ask_k(s0, step + 1);
+    }
+    if (!whole) {                                         // (the scale of a slot that this query does not see may be NaN)
+#pragma unroll
+      for (int j = 0; j < ST; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(ok_here >> j & 1) || here + 16 * j + 4 * grp + i >= limit) {
+            s[j][i] = kNegInf;
+            vs[j][i] = 0.f;
           }
+    }
+    float best = kNegInf;
+#pragma unroll
+    for (int j = 0; j < ST; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) best = fmaxf(best, s[j][i]);
+    const float m_new = fmaxf(m, max_across(best)), base = m_new == kNegInf ? 0.f : m_new;
+    float sum = 0.f, most_w = 0.f;
+#pragma unroll
+    for (int j = 0; j < ST; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = __builtin_amdgcn_exp2f(s[j][i] - base);
+        sum += p;
+        s[j][i] = p * vs[j][i];
+        most_w = fmaxf(most_w, s[j][i]);
+      }
+    most_w = max_across(most_w);
+    const int top_new = max(top, most_w > 0.f ? __builtin_amdgcn_frexp_expf(most_w) : -300);
+    const float alpha = __builtin_amdgcn_exp2f(m - base);
+    l = fmaf(l, alpha, sum);
+    if (__any(top_new != top || m_new != m)) {
+      const float beta = __builtin_amdgcn_ldexpf(alpha, top - top_new);
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= beta;
+    }
+    m = m_new;
+    top = top_new;
+#pragma unroll
+    for (int j = 0; j < ST; j += 2) {
+      f16x8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = __builtin_amdgcn_ldexpf(s[j + i / 4][i % 4], kTop - top);
+        hi[i] = (_Float16)w;
+        lo[i] = (_Float16)(w - (float)hi[i]);
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int u = 0; u < E / 4; u += 2) {
+          const f16x8 v0 = v_halves(word(vc[j][c], u), word(vc[j + 1][c], u)), v1 = v_halves(word(vc[j][c], u + 1), word(vc[j + 1][c], u + 1));
+          f32x4 &o0 = o[c * (E / 4) + u], &o1 = o[c * (E / 4) + u + 1];
+          o0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, hi, o0, 0, 0, 0);
+          o1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, hi, o1, 0, 0, 0);
+          o0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, lo, o0, 0, 0, 0);
+          o1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, lo, o1, 0, 0, 0);
         }
-  }
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    l[t] += __shfl_xor(l[t], 16, 64);
-    l[t] += __shfl_xor(l[t], 32, 64);
-    if (grp == 0) { m_sh[wave][16 * t + col] = m[t]; l_sh[wave][16 * t + col] = l[t]; }
-  }
-  // the waves' partial results, 16 threads to a query
-  constexpr int PER = D / 16;
-  const int c = threadIdx.x / 16, dim0 = threadIdx.x % 16 * PER;
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    if (t) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o_sh[wave][col][16 * i + 4 * grp + e] = __builtin_amdgcn_ldexpf(o[t][i][e], top[t] - kTop);
-    __syncthreads();
-    const int f = first + 16 * t + c;
-    if (f >= queries) continue;
-    float best = kNegInf, sum = 0.f, acc[PER] = {};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) best = fmaxf(best, m_sh[w][16 * t + c]);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float mw = m_sh[w][16 * t + c], lw = l_sh[w][16 * t + c];
-      const float part = mw == kNegInf && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - best);
-      sum = fmaf(part, lw, sum);
-#pragma unroll
-      for (int e = 0; e < PER; ++e) acc[e] = fmaf(part, o_sh[w][c][dim0 + e], acc[e]);
-    }
-    const int r = row0 + f / a.share, h = kvh * a.share + f % a.share;
-    if (a.part) {
-      const size_t rh = (size_t)r * a.n_heads + h;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) a.sums(rh, blockIdx.z, D)[dim0 + e] = acc[e];
-      if (dim0 == 0) *a.stats(rh, blockIdx.z, D) = make_float2(best, sum);
-    } else {
-#pragma unroll
-      for (int e = 0; e < PER; ++e)
-        st<T>::stv((T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + dim0 + e, sum == 0.f ? 0.f : acc[e] / sum);
-    }
-  }
-}
-
-// The chunks' partial results of one row and head, joined by one wave in the chunks' order.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void kv8_join_kernel(Kv8View kv, Kv8Attn a) {
-  constexpr int NP = D > 64 ? D / 64 : 1;
-  const int lane = threadIdx.x & 63, r = blockIdx.x, h = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (h >= a.n_heads) return;
-  const int b = kv8_sequence_of(a.cu_rows, kv.batch, r);
-  if (b >= kv.batch) return;
-  const int n = (a.limit_of(b, r, kv.slots()) + a.chunk - 1) / a.chunk;
-  const size_t rh = (size_t)r * a.n_heads + h;
-  float top = kNegInf;
-  for (int c = lane; c < n; c += 64) top = fmaxf(top, a.stats(rh, c, D)->x);
-  top = wave_max(top);
-  float sum = 0.f, acc[NP] = {};
-  for (int c0 = 0; c0 < n; c0 += 64) {
-    float2 ml = make_float2(kNegInf, 0.f);
-    if (c0 + lane < n) ml = *a.stats(rh, c0 + lane, D);
-    const float w = ml.x == kNegInf && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-    sum += w * ml.y;
-    for (int c = 0; c < min(64, n - c0); ++c) {
-      const float wc = __shfl(w, c, 64);
-      if (lane * NP < D) {
-#pragma unroll
-        for (int e = 0; e < NP; ++e) acc[e] += wc * a.sums(rh, c0 + c, D)[lane * NP + e];
       }
     }
+    if (s0 < end) ask_v();
   }
-  sum = wave_sum(sum);
-  if (lane * NP < D) {
+  // the waves' partial results, 16 threads to a query (addresses from here on are worked out here: computed ahead of the loop, as
+  // the compiler would, they cost it 26 registers that it does not have)
+  int tid = threadIdx.x, share = a.share;
+  asm volatile("" : "+v"(tid), "+s"(share));
+  l = sum_across(l);
+  const int lane_e = tid & 63, col_e = lane_e & 15, grp_e = lane_e >> 4;
+  if (grp_e == 0) { sh.m[wave][col_e] = m; sh.l[wave][col_e] = l; }
 #pragma unroll
-    for (int e = 0; e < NP; ++e)
-      st<T>::stv((T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + lane * NP + e, sum == 0.f ? 0.f : acc[e] / sum);
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sh.o[wave][col_e][16 * i + 4 * grp_e + e] = __builtin_amdgcn_ldexpf(o[i][e], top - kTop);
+  __syncthreads();
+  constexpr int PER = D / 16;
+  const int c = tid / 16, dim0 = tid % 16 * PER, fq = first + c;
+  if (fq >= queries) return;
+  float best = kNegInf, sum = 0.f, acc[PER] = {};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) best = fmaxf(best, sh.m[w][c]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float mw = sh.m[w][c], lw = sh.l[w][c];
+    const float part = mw == kNegInf && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - best);
+    sum = fmaf(part, lw, sum);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = fmaf(part, sh.o[w][c][dim0 + e], acc[e]);
+  }
+  const int r = row0 + fq / a.share, h = kvh * a.share + fq % a.share;
+  if (part >= 0) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) a.sums(part, c, D)[dim0 + e] = acc[e];
+    if (dim0 == 0) *a.stats(part, c, D) = make_float2(best, sum);
+  } else {
+    const int r = row0 + fq / share, h = kvh * share + fq % share;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) st<T>::stv((T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + dim0 + e, acc[e] * inv);
   }
 }
 
-struct Kv8Plan { int qt, tiles, chunk, chunks; };
+template <typename T, int D, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : kResident) void kv8_attention_kernel(Kv8View kv, Kv8Attn a) {
+  __shared__ typename Kv8Segment<T, D, ONCE>::Shared sh;
+  const int lane = threadIdx.x & 63;
+  Kv8Sequence s{0, 0, 0, 0, 1};
+  const int each = kv8_piece(kv, a, s);
+  int u = blockIdx.x, partials = 0;                       // this workgroup's piece, counted from sequence b0's first; partials before it
+  int b = -1, in = 0, pieces = 1;                         // its sequence, its place there, and in how many pieces a segment is cut
+  Kv8Sequence seq{0, 0, 0, 1, 1};
+  for (int b0 = 0; b0 < kv.batch && b < 0; b0 += 64) {
+    if (b0) {
+      if (b0 + lane < kv.batch) s = kv8_sequence(kv, a, b0 + lane);
+      else s.tiles = 0;
+    }
+    const int cut = (s.units + each - 1) / each, n = s.tiles * kv.heads * cut;      // pieces of a segment, of the sequence
+    int upto = n, part = cut > 1 ? n : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o, 64), y = __shfl_up(part, o, 64);
+      if (lane >= o) { upto += x; part += y; }
+    }
+    const uint64_t past = __ballot(upto > u);
+    const int at = past ? __builtin_ffsll((long long)past) - 1 : 63;
+    if (past) {
+      b = b0 + at;
+      seq.row0 = __builtin_amdgcn_readlane(s.row0, at);
+      seq.rows = __builtin_amdgcn_readlane(s.rows, at);
+      seq.len = __builtin_amdgcn_readlane(s.len, at);
+      seq.tiles = __builtin_amdgcn_readlane(s.tiles, at);
+      seq.units = __builtin_amdgcn_readlane(s.units, at);
+      pieces = __builtin_amdgcn_readlane(cut, at);
+      in = u - __builtin_amdgcn_readlane(upto - n, at);
+      partials += __builtin_amdgcn_readlane(part - n, at) + in;
+    } else {
+      u -= __builtin_amdgcn_readlane(upto, 63);
+      partials += __builtin_amdgcn_readlane(part, 63);
+    }
+  }
+  if (b < 0) return;
+  const int segment = in / pieces, i = in % pieces, kvh = segment / seq.tiles, p = pieces > 1 ? partials : -1;
+  if (in < 0 || kvh >= kv.heads || p < -1 || p >= 2 * a.pieces) return;        // (rows that are no prefix sums may overflow the counts)
+  const int u0 = (int)((int64_t)seq.units * i / pieces), u1 = (int)((int64_t)seq.units * (i + 1) / pieces);
+  Kv8Segment<T, D, ONCE>::run(kv, a, sh, b, seq, kvh, segment % seq.tiles * 16, u0 * a.unit, min(seq.len, u1 * a.unit), p);
+}
 
-// How a call is cut: queries per workgroup by how many a sequence has on average, slots per workgroup so that a few thousand
-// workgroups share the work.  Bounds only: the same for every call with the same bounds.
-Kv8Plan kv8_plan(const Kv8View& kv, int d, int dtype, int n_heads, int m_upper, int len_upper) {
+// The partial results of one row and head, joined by one workgroup: D / 4 threads take a partial, the groups of such threads
+// the partials in turn, and the groups' sums are added in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void kv8_join_kernel(Kv8View kv, Kv8Attn a) {
+  constexpr int kGroups = 256 / (D / 4);
+  __shared__ float w_sh[256];
+  __shared__ float4 sum_sh[kGroups][D / 4];
+  const int lane = threadIdx.x & 63, r = blockIdx.x, h = blockIdx.y, group = threadIdx.x / (D / 4), at = threadIdx.x % (D / 4);
+  const int b = __builtin_amdgcn_readfirstlane(kv8_sequence_of(a.cu_rows, kv.batch, r));
+  if (b >= kv.batch) return;
+  Kv8Sequence seq{0, 0, 0, 0, 1};
+  const int each = kv8_piece(kv, a, seq);
+  int before = 0;                                         // partials of the sequences before this one
+  for (int b0 = 0; b0 < kv.batch; b0 += 64) {
+    if (b0 && b0 + lane < kv.batch) seq = kv8_sequence(kv, a, b0 + lane);
+    const int cut = (seq.units + each - 1) / each;
+    before += b0 + lane < b && cut > 1 ? seq.tiles * kv.heads * cut : 0;
+    if (b < b0 + 64) break;
+  }
+  before = wave_sum_int(before);
+  const int row0 = __builtin_amdgcn_readlane(seq.row0, b % 64), tiles = __builtin_amdgcn_readlane(seq.tiles, b % 64);
+  const int n = (__builtin_amdgcn_readlane(seq.units, b % 64) + each - 1) / each;
+  if (n <= 1) return;                                     // written where it was computed
+  const int f = (r - row0) * a.share + h % a.share, col = f % 16;
+  const int p0 = before + (h / a.share * tiles + f / 16) * n;
+  if (r < row0 || before < 0 || p0 < 0 || p0 + n > 2 * a.pieces) return;
+  float best = kNegInf, sum = 0.f;
+  for (int c = lane; c < n; c += 64) best = fmaxf(best, a.stats(p0 + c, col, D)->x);
+  best = wave_max(best);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c0 = 0; c0 < n; c0 += 256) {
+    float w = 0.f;
+    if (c0 + (int)threadIdx.x < n) {
+      const float2 ml = *a.stats(p0 + c0 + threadIdx.x, col, D);
+      w = ml.x == kNegInf && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - best);
+      sum = fmaf(w, ml.y, sum);
+    }
+    if (c0) __syncthreads();
+    w_sh[threadIdx.x] = w;
+    __syncthreads();
+    const int here = min(256, n - c0);
+#pragma unroll 4
+    for (int c = group; c < here; c += kGroups) {
+      const float4 p = reinterpret_cast<const float4*>(a.sums(p0 + c0 + c, col, D))[at];
+      const float wc = w_sh[c];
+      acc.x = fmaf(wc, p.x, acc.x); acc.y = fmaf(wc, p.y, acc.y); acc.z = fmaf(wc, p.z, acc.z); acc.w = fmaf(wc, p.w, acc.w);
+    }
+  }
+  sum_sh[group][at] = acc;
+  __shared__ float l_sh[4];
+  sum = block_sum<256>(sum, l_sh);                        // (its barriers stand between the sums' stores and their loads)
+  if (threadIdx.x >= D / 4) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) {
+    const float4 p = sum_sh[g][at];
+    acc.x += p.x; acc.y += p.y; acc.z += p.z; acc.w += p.w;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* dst = (T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + at * 4;
+  const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+  if constexpr (sizeof(T) == 2) st4(dst, v); else *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
+struct Kv8Plan { int unit, wgs, pieces; bool once, split; };
+
+// By the bounds alone: the same for every call with the same bounds.
+Kv8Plan kv8_plan(const Kv8View& kv, int d, int n_heads, int m_upper, int len_upper) {
   Kv8Plan p;
-  const int64_t queries = (int64_t)m_upper * (n_heads / kv.heads);
-  p.qt = queries > 16 * (int64_t)kv.batch && !(d == 256 && dtype == SL_F32) ? 2 : 1;
   // every sequence rounds its queries up to a tile, and a tile holds one at least
-  const int64_t most = queries / (16 * p.qt) + kv.batch;
-  p.tiles = (int)(queries < most ? queries : most);
-  const int pieces = sl_cdiv(len_upper < 1 ? 1 : len_upper, kWaves * kStep);
-  int want = (int)(4096 / ((int64_t)p.tiles * kv.heads));
-  want = want < 1 ? 1 : want > pieces ? pieces : want;
-  p.chunk = sl_cdiv(pieces, want) * kWaves * kStep;
-  p.chunks = sl_cdiv(len_upper < 1 ? 1 : len_upper, p.chunk);
+  const int64_t queries = (int64_t)m_upper * (n_heads / kv.heads), most = queries / 16 + kv.batch;
+  const int64_t segments = (queries < most ? queries : most) * kv.heads;
+  p.unit = kUnit;
+  while (segments * (len_upper / p.unit + 1) > 1 << 30) p.unit *= 2;          // units are counted in 32 bits
+  const int64_t units = segments * (len_upper / p.unit + 1);
+  p.pieces = kRounds * 256 * (d == 256 ? 2 : kResident);                            // a few rounds of what registers let run at once
+  p.wgs = (int)(units < segments + p.pieces ? units : segments + p.pieces);
+  p.split = len_upper > p.unit * kLeast;
+  p.once = queries <= 16 * (int64_t)kv.batch;
   return p;
 }
 
@@ -415,24 +519,22 @@ Kv8Plan kv8_plan(const Kv8View& kv, int d, int dtype, int n_heads, int m_upper, 
 
 size_t slk_kv8_attention_bytes(const Kv8View& kv, int d, int n_heads, int m_upper, int len_upper) {
   if (m_upper == 0) return 256;
-  int chunks = 1;                                         // of either type of queries
-  for (int dtype : {SL_F32, SL_BF16}) chunks = max(chunks, kv8_plan(kv, d, dtype, n_heads, m_upper, len_upper).chunks);
-  return chunks == 1 ? 256 : sl_align_up((size_t)m_upper * n_heads * chunks * (d + 2) * sizeof(float), 256);
+  const Kv8Plan p = kv8_plan(kv, d, n_heads, m_upper, len_upper);
+  return p.split ? sl_align_up((size_t)p.pieces * 32 * (d + 2) * sizeof(float), 256) : 256;
 }
 
 int slk_kv8_attention(hipStream_t s, const Kv8View& kv, int d, int dtype, const void* q, int64_t q_stride, int n_heads,
                       const int32_t* cu_rows, const int32_t* seq_len, const int32_t* row_len, int m_upper, int len_upper, float scale,
                       void* out, int64_t out_stride, void* workspace) {
-  const Kv8Plan p = kv8_plan(kv, d, dtype, n_heads, m_upper, len_upper);
-  const Kv8Attn a{q, out, p.chunks == 1 ? nullptr : (float*)workspace, cu_rows, seq_len, row_len, q_stride, out_stride, n_heads,
-                  n_heads / kv.heads, m_upper, len_upper, p.chunk, p.chunks, (float)((double)scale * 1.4426950408889634)};
-  const dim3 grid(p.tiles, kv.heads, p.chunks), join(m_upper, sl_cdiv(n_heads, 4));
-#define KV8_CALL(T, D)                                                                                           \
-  do {                                                                                                           \
-    constexpr int kMost = sizeof(T) == 4 && D == 256 ? 1 : 2;                                                    \
-    if (p.qt == 1) hipLaunchKernelGGL((kv8_attention_kernel<T, D, 1>), grid, dim3(64 * kWaves), 0, s, kv, a);    \
-    else hipLaunchKernelGGL((kv8_attention_kernel<T, D, kMost>), grid, dim3(64 * kWaves), 0, s, kv, a);          \
-    if (a.part) hipLaunchKernelGGL((kv8_join_kernel<T, D>), join, dim3(256), 0, s, kv, a);                       \
+  const Kv8Plan p = kv8_plan(kv, d, n_heads, m_upper, len_upper);
+  const Kv8Attn a{q, out, (float*)workspace, cu_rows, seq_len, row_len, q_stride, out_stride, n_heads, n_heads / kv.heads, m_upper,
+                  len_upper, p.unit, p.pieces, (float)((double)scale * 1.4426950408889634)};
+  const dim3 join(m_upper, n_heads);
+#define KV8_CALL(T, D)                                                                                                  \
+  do {                                                                                                                  \
+    if (p.once) hipLaunchKernelGGL((kv8_attention_kernel<T, D, true>), dim3(p.wgs), dim3(64 * kWaves), 0, s, kv, a);    \
+    else hipLaunchKernelGGL((kv8_attention_kernel<T, D, false>), dim3(p.wgs), dim3(64 * kWaves), 0, s, kv, a);          \
+    if (p.split) hipLaunchKernelGGL((kv8_join_kernel<T, D>), join, dim3(256), 0, s, kv, a);                             \
   } while (0)
 #define KV8_BY_HEAD(T)                 \
   switch (d) {                         \
