@@ -92,66 +92,130 @@ __device__ inline bf16x8 q4_to_bf16(uint32_t w) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 
-// One workgroup: 16 columns, 16 MT rows; its waves take the 128-deep blocks of the reduction in turn and add up in LDS.
-template <int GS, int MT>
+// One workgroup: 16 CT columns, 16 MT rows; its waves take the 128-deep blocks of the reduction in turn and add up in LDS.
+//
+// Rows pass through LDS, each wave's through a part of its own: an operand has 16 rows side by side in a wave's lanes, and loaded
+// so from row-major memory every lane is an access of its own (16 bytes a cycle of the address unit, which was busy 70 to 88 % of
+// the time).  Here eight lanes take a row's 128 consecutive bytes and the operand is read back from LDS; 16-byte
+// pieces of a row that would meet in one bank are kept apart by an exclusive or of their row with their place.
+// A wave asks for a block's weights and rows one block ahead.
+template <int GS, int MT, int CT>
 __global__ __launch_bounds__(64 * kWaves) void q4_linear_kernel(const bf16_t* x, const unsigned char* packed, const int32_t* m_dev, int m_upper,
                                                                 int n, int k, float* y_f32, bf16_t* y_bf16, const int32_t* row_map) {
-  constexpr int kBlock = q4_block_bytes(32 * GS);
-  __shared__ float sh[kWaves][16 * MT][kCols + 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, grp = lane >> 4;
+  constexpr int kBlock = q4_block_bytes(32 * GS), kGroups = 4 / GS;
+  constexpr int kSumBytes = kWaves * 16 * (16 * CT + 4) * 4, kRowBytes = kWaves * MT * 4096;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kSumBytes > kRowBytes ? kSumBytes : kRowBytes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
   const int m = min(*m_dev, m_upper), m0 = blockIdx.y * 16 * MT;
   if (m0 >= m) return;
-  const int blocks_k = (k + kDepth - 1) / kDepth;
-  const unsigned char* wp = packed + (size_t)blockIdx.x * blocks_k * kBlock;
-  const bf16_t* xr[MT];
+  const int blocks_k = (k + kDepth - 1) / kDepth, tiles_n = (n + kCols - 1) / kCols;
+  const unsigned char* wp[CT];                            // (a tile of columns past the last one is read as the last and not stored)
 #pragma unroll
-  for (int t = 0; t < MT; ++t) xr[t] = x + (size_t)min(m0 + 16 * t + col, m - 1) * k;
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)1.f;
-  f32x4 y[MT] = {};
-  for (int kb = wave; kb < blocks_k; kb += kWaves) {
-    const uint4 c4 = reinterpret_cast<const uint4*>(wp + (size_t)kb * kBlock)[lane];
-    const uint32_t c[4] = {c4.x, c4.y, c4.z, c4.w};
-#pragma unroll
-    for (int j = 0; j < 4; j += GS) {
-      f32x4 acc[MT] = {}, sum[MT] = {};
-#pragma unroll
-      for (int i = 0; i < GS; ++i) {
-        const bf16x8 wf = q4_to_bf16(c[j + i]);
-        const int at = kb * kDepth + (j + i) * 32 + grp * 8;
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          bf16x8 xf = {};
-          if (at < k) xf = *reinterpret_cast<const bf16x8*>(xr[t] + at);
-          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf, acc[t], 0, 0, 0);
-          sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xf, sum[t], 0, 0, 0);
-        }
-      }
-      const uint4 p = reinterpret_cast<const uint4*>(wp + (size_t)kb * kBlock + kCodeBytes + j / GS * kCols * 4)[grp];
-      const uint32_t ps[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          y[t][e] = fmaf(__uint_as_float(ps[e] & 0xffff0000u), fmaf(-__uint_as_float(ps[e] << 16), sum[t][e], acc[t][e]), y[t][e]);
-    }
-  }
+  for (int c = 0; c < CT; ++c) wp[c] = packed + (size_t)min((int)blockIdx.x * CT + c, tiles_n - 1) * blocks_k * kBlock;
+  // loads of rows: lane l takes piece l % 8 (8 numbers) of row l / 8, four loads to 16 rows of a block
+  const bf16_t* xr[MT][2];
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sh[wave][16 * t + col][4 * grp + e] = y[t][e];
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * MT * kCols; i += 64 * kWaves) {
-    const int r = m0 + i / kCols, c = blockIdx.x * kCols + i % kCols;
-    if (r >= m || c >= n) continue;
-    float v = 0.f;
+    for (int i = 0; i < 2; ++i) xr[t][i] = x + (size_t)min(m0 + 16 * t + 8 * i + (lane >> 3), m - 1) * k + (lane & 7) * 8;
+  unsigned char* mine = lds + wave * (MT * 4096);
+  const int put = ((lane & 3) * 16 + ((lane >> 3) ^ (lane & 7))) * 16 + (lane >> 2 & 1) * 1024;     // of rows 0 .. 7; rows 8 .. 15 at put ^ 128
+  const int get0 = (grp * 16 + (col ^ grp)) * 16, get1 = (grp * 16 + (col ^ (grp + 4))) * 16;       // of even and odd products
+
+  uint4 w[CT], wn[CT], p[CT][kGroups], pn[CT][kGroups], xn[MT][4];
+  auto ask = [&](int kb) {
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += sh[w][i / kCols][i % kCols];
-    if (y_f32) y_f32[(size_t)r * n + c] = v;
-    else y_bf16[(size_t)(row_map ? row_map[r] : r) * n + c] = (bf16_t)v;
+    for (int c = 0; c < CT; ++c) {
+      const unsigned char* b = wp[c] + (size_t)kb * kBlock;
+      wn[c] = reinterpret_cast<const uint4*>(b)[lane];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) pn[c][g] = reinterpret_cast<const uint4*>(b + kCodeBytes + g * kCols * 4)[grp];
+    }
+    const int at = kb * kDepth;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {                       // k is a multiple of 8: a lane's 8 numbers are all there or none
+        const int d = at + i / 2 * 64;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (at + kDepth <= k || d + (lane & 7) * 8 < k) v = *reinterpret_cast<const uint4*>(xr[t][i % 2] + d);
+        xn[t][i] = v;
+      }
+  };
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)1.f;
+  f32x4 y[MT][CT] = {};
+  int kb = wave;
+  if (kb < blocks_k) ask(kb);
+  for (; kb < blocks_k; kb += kWaves) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      w[c] = wn[c];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) p[c][g] = pn[c][g];
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(mine + t * 4096 + i / 2 * 2048 + (i % 2 ? put ^ 128 : put)) = xn[t][i];
+    if (kb + kWaves < blocks_k) ask(kb + kWaves);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      f32x4 acc[MT][CT], sum[MT];
+#pragma unroll
+      for (int i = 0; i < GS; ++i) {
+        const int j = g * GS + i;
+        bf16x8 wf[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) wf[c] = q4_to_bf16(j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w);
+        const f32x4 zero = {};
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          const bf16x8 xf = *reinterpret_cast<const bf16x8*>(mine + t * 4096 + j * 1024 + (j % 2 ? get1 : get0));
+          sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xf, i ? sum[t] : zero, 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c], xf, i ? acc[t][c] : zero, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const uint32_t ps[4] = {p[c][g].x, p[c][g].y, p[c][g].z, p[c][g].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float scale = __uint_as_float(ps[e] & 0xffff0000u), z = __uint_as_float(ps[e] << 16);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) y[t][c][e] = fmaf(scale, fmaf(-z, sum[t][e], acc[t][c][e]), y[t][c][e]);
+        }
+      }
+    }
+  }
+  auto sh = reinterpret_cast<float(*)[16][16 * CT + 4]>(lds);      // [wave][row][column]
+  __syncthreads();
+  const int first = blockIdx.x * 16 * CT;
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    if (m0 + 16 * t >= m) break;
+    if (t) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(&sh[wave][col][16 * c + 4 * grp]) = y[t][c];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 64 * CT; i += 64 * kWaves) {
+      const int r = m0 + 16 * t + i / (4 * CT), c = i % (4 * CT) * 4;
+      if (r >= m || first + c >= n) continue;
+      f32x4 v = {};
+#pragma unroll
+      for (int s = 0; s < kWaves; ++s) v += *reinterpret_cast<const f32x4*>(&sh[s][i / (4 * CT)][c]);
+      const size_t at = (size_t)(row_map ? row_map[r] : r) * n + first + c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (first + c + e < n) {
+          if (y_f32) y_f32[at + e] = v[e];
+          else y_bf16[at + e] = (bf16_t)v[e];
+        }
+    }
   }
 }
 
@@ -183,17 +247,28 @@ int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int g
 
 int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
                   void* y_bf16, const int32_t* row_map) {
-  const int mt = m_upper <= 16 ? 1 : m_upper <= 32 ? 2 : 4;
-  const dim3 grid(sl_cdiv(n, kCols), sl_cdiv(m_upper, 16 * mt));
-#define Q4_CALL(GS, MT)                                                                                                                      \
-  hipLaunchKernelGGL((q4_linear_kernel<GS, MT>), grid, dim3(64 * kWaves), 0, s, (const bf16_t*)x, (const unsigned char*)packed, m_dev, m_upper, \
+  const int tiles = sl_cdiv(m_upper, 16);
+#ifndef FM
+  int mt = tiles >= 2 ? 2 : 1, ct = 2;
+#else
+  int mt = FM, ct = FC;
+#endif
+  const dim3 grid(sl_cdiv(n, kCols * ct), sl_cdiv(m_upper, 16 * mt));
+#define Q4_CALL(GS, MT, CT)                                                                                                                      \
+  hipLaunchKernelGGL((q4_linear_kernel<GS, MT, CT>), grid, dim3(64 * kWaves), 0, s, (const bf16_t*)x, (const unsigned char*)packed, m_dev, m_upper, \
                      n, k, y_f32, (bf16_t*)y_bf16, row_map)
-#define Q4_BY_ROWS(GS)                                                                      \
-  do {                                                                                      \
-    if (mt == 1) Q4_CALL(GS, 1); else if (mt == 2) Q4_CALL(GS, 2); else Q4_CALL(GS, 4);     \
+#define Q4_BY_TILE(GS)                             \
+  do {                                             \
+    if (mt == 1 && ct == 1) Q4_CALL(GS, 1, 1);     \
+    else if (mt == 1 && ct == 2) Q4_CALL(GS, 1, 2); \
+    else if (mt == 1) Q4_CALL(GS, 1, 4);           \
+    else if (mt == 2 && ct == 1) Q4_CALL(GS, 2, 1); \
+    else if (mt == 2 && ct == 2) Q4_CALL(GS, 2, 2); \
+    else if (mt == 2) Q4_CALL(GS, 2, 4);           \
+    else Q4_CALL(GS, 4, 2);                        \
   } while (0)
-  if (group == 32) Q4_BY_ROWS(1); else if (group == 64) Q4_BY_ROWS(2); else Q4_BY_ROWS(4);
-#undef Q4_BY_ROWS
+  if (group == 32) Q4_BY_TILE(1); else if (group == 64) Q4_BY_TILE(2); else Q4_BY_TILE(4);
+#undef Q4_BY_TILE
 #undef Q4_CALL
   SL_LAUNCH_CHECK();
   return SL_OK;
