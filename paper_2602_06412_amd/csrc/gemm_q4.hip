@@ -92,122 +92,161 @@ __device__ inline bf16x8 q4_to_bf16(uint32_t w) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-constexpr int kWaves = 8;
+// sum over the 4 or 8 neighbouring lanes that hold one row's pieces, in all of them
+template <int N>
+__device__ inline float sum_neighbours(float v) {
+  v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0xB1, 15, 15, true));          // lane ^ 1
+  v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x4E, 15, 15, true));          // lane ^ 2
+  if (N == 8) v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x141, 15, 15, true));      // 7 - lane, of 8
+  return v;
+}
+__device__ inline float sum_of_piece(const uint4& v) {
+  const bf16x2 one = {(bf16_t)1.f, (bf16_t)1.f};
+  float s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v.x), one, 0.f, false);
+  s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v.y), one, s, false);
+  s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v.z), one, s, false);
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v.w), one, s, false);
+}
 
-// One workgroup: 16 CT columns, 16 MT rows; its waves take the 128-deep blocks of the reduction in turn and add up in LDS.
+// One workgroup: 16 MT rows, WN waves side by side of 16 CT columns each, WK such groups along the reduction, which add up in LDS
+// at the end.  A wave asks U blocks (128 deep) of its group ahead for weights and rows.
 //
-// Rows pass through LDS, each wave's through a part of its own: an operand has 16 rows side by side in a wave's lanes, and loaded
-// so from row-major memory every lane is an access of its own (16 bytes a cycle of the address unit, which was busy 70 to 88 % of
-// the time).  Here eight lanes take a row's 128 consecutive bytes and the operand is read back from LDS; 16-byte
-// pieces of a row that would meet in one bank are kept apart by an exclusive or of their row with their place.
-// A wave asks for a block's weights and rows one block ahead.
-template <int GS, int MT, int CT>
-__global__ __launch_bounds__(64 * kWaves) void q4_linear_kernel(const bf16_t* x, const unsigned char* packed, const int32_t* m_dev, int m_upper,
-                                                                int n, int k, float* y_f32, bf16_t* y_bf16, const int32_t* row_map) {
-  constexpr int kBlock = q4_block_bytes(32 * GS), kGroups = 4 / GS;
-  constexpr int kSumBytes = kWaves * 16 * (16 * CT + 4) * 4, kRowBytes = kWaves * MT * 4096;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[kSumBytes > kRowBytes ? kSumBytes : kRowBytes];
+// Rows pass through LDS, once for the WN waves of a group, and with them goes the sum of each group of weights' inputs.  An
+// operand has 16 rows side by side in a wave's lanes, and loaded so from row-major memory every lane is an access of its own (16
+// bytes a cycle of the address unit, which was busy 70 to 88 % of the time: 61 rows, n = 4096, k = 12288 took 53 us for 33).  Here eight
+// lanes take a row's 128 consecutive bytes; 16-byte pieces that would meet in one bank are kept apart by an exclusive or of their row
+// with their place.
+template <int GS, int MT, int CT, int WN, int WK, int U>
+__global__ __launch_bounds__(64 * WN * WK) void q4_linear_kernel(const bf16_t* x, const unsigned char* packed, const int32_t* m_dev, int m_upper, int n,
+                                                               int k, float* y_f32, bf16_t* y_bf16, const int32_t* row_map) {
+  constexpr int kBlock = q4_block_bytes(32 * GS), kGroups = 4 / GS, kUnits = (MT * 2 + WN - 1) / WN, kWidth = 16 * CT * WN;
+  constexpr int kBufs = WN > 1 ? 2 : 1;                   // a group of several waves writes one while the other is read
+  constexpr int kRowBytes = WK * kBufs * MT * 4096, kSumBytes = WK * 16 * (kWidth + 4) * 4;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kRowBytes > kSumBytes ? kRowBytes : kSumBytes];
+  __shared__ float sums[WK][kBufs][kGroups][16 * MT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4;
+  const int wn = wave % WN, wk = wave / WN;
   const int m = min(*m_dev, m_upper), m0 = blockIdx.y * 16 * MT;
   if (m0 >= m) return;
   const int blocks_k = (k + kDepth - 1) / kDepth, tiles_n = (n + kCols - 1) / kCols;
   const unsigned char* wp[CT];                            // (a tile of columns past the last one is read as the last and not stored)
 #pragma unroll
-  for (int c = 0; c < CT; ++c) wp[c] = packed + (size_t)min((int)blockIdx.x * CT + c, tiles_n - 1) * blocks_k * kBlock;
-  // loads of rows: lane l takes piece l % 8 (8 numbers) of row l / 8, four loads to 16 rows of a block
-  const bf16_t* xr[MT][2];
+  for (int c = 0; c < CT; ++c) wp[c] = packed + (size_t)min((int)(blockIdx.x * WN + wn) * CT + c, tiles_n - 1) * blocks_k * kBlock;
+  const int put = ((lane & 3) * 16 + ((lane >> 3) ^ (lane & 7))) * 16 + (lane >> 2 & 1) * 1024;     // as below, rows 0 .. 7
+  const int get0 = (grp * 16 + (col ^ grp)) * 16, get1 = (grp * 16 + (col ^ (grp + 4))) * 16;
+  // a wave's share of the rows: 8 rows q % 2 of tile q / 2, eight lanes to 128 bytes of a row.  Rows past the count are read as the
+  // last one (they end in results that are not stored), pieces past k as the last one and then cleared
+  const bf16_t* xr[kUnits];
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) xr[t][i] = x + (size_t)min(m0 + 16 * t + 8 * i + (lane >> 3), m - 1) * k + (lane & 7) * 8;
-  unsigned char* mine = lds + wave * (MT * 4096);
-  const int put = ((lane & 3) * 16 + ((lane >> 3) ^ (lane & 7))) * 16 + (lane >> 2 & 1) * 1024;     // of rows 0 .. 7; rows 8 .. 15 at put ^ 128
-  const int get0 = (grp * 16 + (col ^ grp)) * 16, get1 = (grp * 16 + (col ^ (grp + 4))) * 16;       // of even and odd products
-
-  uint4 w[CT], wn[CT], p[CT][kGroups], pn[CT][kGroups], xn[MT][4];
-  auto ask = [&](int kb) {
+  for (int u = 0; u < kUnits; ++u) xr[u] = x + (size_t)min(m0 + 8 * (wn + u * WN) + (lane >> 3), m - 1) * k + (lane & 7) * 8;
+  uint4 w[U][CT], p[U][CT][kGroups], xn[U][kUnits][2];
+  auto ask = [&](int s, int kb) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const unsigned char* b = wp[c] + (size_t)kb * kBlock;
-      wn[c] = reinterpret_cast<const uint4*>(b)[lane];
+      w[s][c] = reinterpret_cast<const uint4*>(b)[lane];
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) pn[c][g] = reinterpret_cast<const uint4*>(b + kCodeBytes + g * kCols * 4)[grp];
+      for (int g = 0; g < kGroups; ++g) p[s][c][g] = reinterpret_cast<const uint4*>(b + kCodeBytes + g * kCols * 4)[grp];
     }
-    const int at = kb * kDepth;
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {                       // k is a multiple of 8: a lane's 8 numbers are all there or none
-        const int d = at + i / 2 * 64;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (at + kDepth <= k || d + (lane & 7) * 8 < k) v = *reinterpret_cast<const uint4*>(xr[t][i % 2] + d);
-        xn[t][i] = v;
-      }
+    for (int u = 0; u < kUnits; ++u) {
+      xn[s][u][0] = *reinterpret_cast<const uint4*>(xr[u] + min(kb * kDepth, k - 8 - (lane & 7) * 8));
+      xn[s][u][1] = *reinterpret_cast<const uint4*>(xr[u] + min(kb * kDepth + 64, k - 8 - (lane & 7) * 8));
+    }
   };
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (bf16_t)1.f;
   f32x4 y[MT][CT] = {};
-  int kb = wave;
-  if (kb < blocks_k) ask(kb);
-  for (; kb < blocks_k; kb += kWaves) {
+  const int steps = (blocks_k + WK - 1) / WK;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      w[c] = wn[c];
+  for (int s = 0; s < U; ++s)
+    ask(s, min(s * WK + wk, blocks_k - 1));
+  for (int it0 = 0; it0 < steps; it0 += U)
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) p[c][g] = pn[c][g];
+  for (int s = 0; s < U; ++s) {
+    const int it = it0 + s, kb = it * WK + wk;
+    if (it >= steps) break;
+    unsigned char* buf = lds + (wk * kBufs + it % kBufs) * (MT * 4096);
+    if (kb * kDepth + kDepth > k) {                       // the last block, or one past it
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (kb * kDepth + 64 * i + (lane & 7) * 8 >= k) xn[s][u][i] = make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(mine + t * 4096 + i / 2 * 2048 + (i % 2 ? put ^ 128 : put)) = xn[t][i];
-    if (kb + kWaves < blocks_k) ask(kb + kWaves);
+      for (int u = 0; u < kUnits; ++u) {
+        const int q = wn + u * WN;
+        if (2 * MT % WN == 0 || q < 2 * MT) {
+          unsigned char* dst = buf + q / 2 * 4096 + (q % 2 ? put ^ 128 : put);
+          *reinterpret_cast<uint4*>(dst) = xn[s][u][0];
+          *reinterpret_cast<uint4*>(dst + 2048) = xn[s][u][1];
+          const float a = sum_of_piece(xn[s][u][0]), b = sum_of_piece(xn[s][u][1]);
+          float* to = &sums[wk][it % kBufs][0][8 * q + (lane >> 3)];
+          if (GS == 4) {
+            const float v = sum_neighbours<8>(a + b);
+            if ((lane & 7) == 0) to[0] = v;
+          } else if (GS == 2) {
+            const float v = sum_neighbours<8>(a), v2 = sum_neighbours<8>(b);
+            if ((lane & 7) == 0) { to[0] = v; to[16 * MT] = v2; }
+          } else {
+            const float v = sum_neighbours<4>(a), v2 = sum_neighbours<4>(b);
+            if ((lane & 3) == 0) { to[(lane >> 2 & 1) * 16 * MT] = v; to[(2 + (lane >> 2 & 1)) * 16 * MT] = v2; }
+          }
+        }
+      }
+    if (WN > 1) {
+      __syncthreads();
+    } else {                                              // rows of the wave's own: LDS serves a wave in order
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      f32x4 acc[MT][CT], sum[MT];
+      f32x4 acc[MT][CT];
 #pragma unroll
       for (int i = 0; i < GS; ++i) {
         const int j = g * GS + i;
         bf16x8 wf[CT];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) wf[c] = q4_to_bf16(j == 0 ? w[c].x : j == 1 ? w[c].y : j == 2 ? w[c].z : w[c].w);
+        for (int c = 0; c < CT; ++c) wf[c] = q4_to_bf16(j == 0 ? w[s][c].x : j == 1 ? w[s][c].y : j == 2 ? w[s][c].z : w[s][c].w);
         const f32x4 zero = {};
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          const bf16x8 xf = *reinterpret_cast<const bf16x8*>(mine + t * 4096 + j * 1024 + (j % 2 ? get1 : get0));
-          sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, xf, i ? sum[t] : zero, 0, 0, 0);
+          const bf16x8 xf = *reinterpret_cast<const bf16x8*>(buf + t * 4096 + j * 1024 + (j % 2 ? get1 : get0));
 #pragma unroll
           for (int c = 0; c < CT; ++c) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[c], xf, i ? acc[t][c] : zero, 0, 0, 0);
         }
       }
+      float sx[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) sx[t] = sums[wk][it % kBufs][g][16 * t + col];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const uint32_t ps[4] = {p[c][g].x, p[c][g].y, p[c][g].z, p[c][g].w};
+        const uint32_t ps[4] = {p[s][c][g].x, p[s][c][g].y, p[s][c][g].z, p[s][c][g].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float scale = __uint_as_float(ps[e] & 0xffff0000u), z = __uint_as_float(ps[e] << 16);
 #pragma unroll
-          for (int t = 0; t < MT; ++t) y[t][c][e] = fmaf(scale, fmaf(-z, sum[t][e], acc[t][c][e]), y[t][c][e]);
+          for (int t = 0; t < MT; ++t) y[t][c][e] = fmaf(scale, fmaf(-z, sx[t], acc[t][c][e]), y[t][c][e]);
         }
       }
     }
+    ask(s, min(kb + U * WK, blocks_k - 1));
   }
-  auto sh = reinterpret_cast<float(*)[16][16 * CT + 4]>(lds);      // [wave][row][column]
-  __syncthreads();
-  const int first = blockIdx.x * 16 * CT;
+  auto sh = reinterpret_cast<float(*)[16][kWidth + 4]>(lds);
+  const int first = blockIdx.x * kWidth;
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
     if (m0 + 16 * t >= m) break;
-    if (t) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(&sh[wave][col][16 * c + 4 * grp]) = y[t][c];
     __syncthreads();
-    for (int i = threadIdx.x; i < 64 * CT; i += 64 * kWaves) {
-      const int r = m0 + 16 * t + i / (4 * CT), c = i % (4 * CT) * 4;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4*>(&sh[wk][col][(wn * CT + c) * 16 + 4 * grp]) = y[t][c];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * kWidth; i += 64 * WN * WK) {
+      const int r = m0 + 16 * t + i / (kWidth / 4), c = i % (kWidth / 4) * 4;
       if (r >= m || first + c >= n) continue;
       f32x4 v = {};
 #pragma unroll
-      for (int s = 0; s < kWaves; ++s) v += *reinterpret_cast<const f32x4*>(&sh[s][i / (4 * CT)][c]);
+      for (int s = 0; s < WK; ++s) v += *reinterpret_cast<const f32x4*>(&sh[s][i / (kWidth / 4)][c]);
       const size_t at = (size_t)(row_map ? row_map[r] : r) * n + first + c;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -247,29 +286,35 @@ int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int g
 
 int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
                   void* y_bf16, const int32_t* row_map) {
-  const int tiles = sl_cdiv(m_upper, 16);
-#ifndef FM
-  int mt = tiles >= 2 ? 2 : 1, ct = 2;
-#else
-  int mt = FM, ct = FC;
-#endif
-  const dim3 grid(sl_cdiv(n, kCols * ct), sl_cdiv(m_upper, 16 * mt));
-#define Q4_CALL(GS, MT, CT)                                                                                                                      \
-  hipLaunchKernelGGL((q4_linear_kernel<GS, MT, CT>), grid, dim3(64 * kWaves), 0, s, (const bf16_t*)x, (const unsigned char*)packed, m_dev, m_upper, \
-                     n, k, y_f32, (bf16_t*)y_bf16, row_map)
-#define Q4_BY_TILE(GS)                             \
-  do {                                             \
-    if (mt == 1 && ct == 1) Q4_CALL(GS, 1, 1);     \
-    else if (mt == 1 && ct == 2) Q4_CALL(GS, 1, 2); \
-    else if (mt == 1) Q4_CALL(GS, 1, 4);           \
-    else if (mt == 2 && ct == 1) Q4_CALL(GS, 2, 1); \
-    else if (mt == 2 && ct == 2) Q4_CALL(GS, 2, 2); \
-    else if (mt == 2) Q4_CALL(GS, 2, 4);           \
-    else Q4_CALL(GS, 4, 2);                        \
+  // Tiles, us by tile (rows x columns, waves side by side x along the reduction; "-" not measured with that one alone):
+  //   n, k, rows            16x16,1x16  16x32,1x8  16x48,1x8  32x32,1x8  32x128,4x2
+  //   4096, 4096, 1             6.5        7.7        8.4        9.5        18
+  //   4096, 12288, 16          11.7       15.7       19.2       21.7        58
+  //   12288, 4096, 16          13.5       10.7        9.9       14.0        19
+  //   24576, 4096, 8           21.6       13.5       13.3       18.5        19
+  //   4096, 4096, 32            9.5        7.7        9.0        9.9        18
+  //   4096, 12288, 61          37.6       26.7       31.1       23.9        58
+  //   12288, 4096, 100         65         36         34         33          28
+  //   24576, 4096, 224        256        136        126        114          81
+  // Few rows are a matter of the weights' latency: workgroups enough for all CUs, many waves along the reduction, and as many columns as
+  // still leave one workgroup to a CU.  Many rows are a matter of unpacking weights and of moving rows: a large tile whose waves share
+  // them, once there are enough of it.
+  const int rows16 = sl_cdiv(m_upper, 16), tiles_n = sl_cdiv(n, kCols), blocks_k = sl_cdiv(k, kDepth);
+#define Q4_RUN(GS, MT, CT, WN, WK, U)                                                                                                  \
+  hipLaunchKernelGGL((q4_linear_kernel<GS, MT, CT, WN, WK, U>), dim3(sl_cdiv(n, kCols * CT * WN), sl_cdiv(m_upper, 16 * MT)),          \
+                     dim3(64 * WN * WK), 0, s, (const bf16_t*)x, (const unsigned char*)packed, m_dev, m_upper, n, k, y_f32,             \
+                     (bf16_t*)y_bf16, row_map)
+#define Q4_BY_TILE(GS)                                                                                                                 \
+  do {                                                                                                                                 \
+    if (rows16 >= 3 && sl_cdiv(n, 128) * sl_cdiv(m_upper, 32) >= 192) Q4_RUN(GS, 2, 2, 4, 2, 2);                                       \
+    else if (rows16 >= 3) Q4_RUN(GS, 2, 2, 1, 8, 1);                                                                                   \
+    else if (rows16 == 1 && tiles_n <= 256 && blocks_k >= 16) Q4_RUN(GS, 1, 1, 1, 16, 1);                                              \
+    else if (tiles_n * rows16 <= 512) Q4_RUN(GS, 1, 2, 1, 8, 1);                                                                       \
+    else Q4_RUN(GS, 1, 3, 1, 8, 1);                                                                                                    \
   } while (0)
   if (group == 32) Q4_BY_TILE(1); else if (group == 64) Q4_BY_TILE(2); else Q4_BY_TILE(4);
 #undef Q4_BY_TILE
-#undef Q4_CALL
+#undef Q4_RUN
   SL_LAUNCH_CHECK();
   return SL_OK;
 }
