@@ -7,9 +7,10 @@
 // order in which the matrix cores take them (16-row products, lane l: row l % 16, the (l / 16)-th quarter of the reduction), so a
 // lane's share of an operand is one load of 16 bytes (8 with d = 32) and a wave's load is one contiguous KiB:
 //   K  [d / 4E][4][16 slots][E dims]            signed bytes, E = 16 (8 with d = 32): the operand of a product of 8-bit integers
-//   V  [d / 4E][4][16 dims][E / 4][4 slots]     code + 128; reduction over slots: the scores' product K Q^T leaves slots
+//   V  [d / 4E][4][16][E / 4 dims][4 slots]     code + 128; reduction over slots: the scores' product K Q^T leaves slots
 //                                               4 (l / 16) .. + 3 of a tile in lane l, so probabilities become the second
-//                                               product's operand in place
+//                                               product's operand in place; a lane's E / 4 dims are neighbours, one in each of
+//                                               as many products, so that a block of neighbouring dims and slots is one store
 #pragma once
 #include "sl_common.h"
 
@@ -22,7 +23,7 @@ struct Kv8Tile {
     return ((dim / (4 * E)) * 64 + (dim % (4 * E)) / E * 16 + slot) * E + dim % E;
   }
   __host__ __device__ static constexpr int v_at(int slot, int dim) {
-    return kV + ((dim / (4 * E)) * 64 + slot / 4 * 16 + dim % 16) * E + (dim % (4 * E)) / 16 * 4 + slot % 4;
+    return kV + ((dim / (4 * E)) * 64 + slot / 4 * 16 + dim % (4 * E) / (E / 4)) * E + dim % (E / 4) * 4 + slot % 4;
   }
 };
 

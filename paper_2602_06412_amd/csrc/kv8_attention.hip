@@ -6,8 +6,8 @@
 // of the matrix products: S^T = K Q^T (16 slots x 16 queries) and O^T = V^T P^T.  S^T leaves in lane l the scores of query l % 16
 // and slots 4 (l / 16) .. + 3 of a tile, which is the operand the second product wants, so probabilities never leave registers.
 //
-// Unpacking codes is what such a kernel would spend its time on: an integer-to-float conversion costs a wave four times an
-// addition, and with K and V converted to bf16 the largest case took 291 us, 180 as follows (memory alone 170 at that stage):
+// Unpacking codes is what such a kernel would spend its instructions on: with K and V converted to bf16, 1.5 a number, the largest
+// case took 291 us, 180 as follows (its loads alone 170 at that stage):
 //   K is not unpacked: the product is one of 8-bit integers, the query being a fixed-point number of three signed bytes,
 //     q = 2^(e - 22) (65536 a + 256 b + c), 2^(e-1) <= max|q| < 2^e: 23 bits of the row's largest number, as good as fp32's own sums.
 //     Each byte's product starts from the integer 0x4B400000, whose bits are the float 1.5 * 2^23, so that the result, below 2^22
@@ -358,9 +358,12 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
   const int lane_e = tid & 63, col_e = lane_e & 15, grp_e = lane_e >> 4;
   if (grp_e == 0) { sh.m[wave][col_e] = m; sh.l[wave][col_e] = l; }
 #pragma unroll
-  for (int i = 0; i < DT; ++i)
+  for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sh.o[wave][col_e][16 * i + 4 * grp_e + e] = __builtin_amdgcn_ldexpf(o[i][e], top - kTop);
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int u = 0; u < E / 4; ++u)                     // dims (E / 4) row + u of the chunk
+        sh.o[wave][col_e][c * 4 * E + E / 4 * (4 * grp_e + e) + u] = __builtin_amdgcn_ldexpf(o[c * (E / 4) + u][e], top - kTop);
   __syncthreads();
   constexpr int PER = D / 16;
   const int c = tid / 16, dim0 = tid % 16 * PER, fq = first + c;

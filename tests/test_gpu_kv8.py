@@ -194,6 +194,23 @@ def test_of_adjacent_rows_with_one_slot_the_last_is_kept():
     assert torch.equal(k.cpu(), want) and torch.equal(v.cpu(), -want)
 
 
+@pytest.mark.parametrize("heads", [1, 3])
+def test_many_rows_that_name_one_quad(heads):
+    """Longer than a wave: 64, 65 and 200 adjacent rows on one slot, and on the slots of one quad in turn."""
+    d, m = 64, 329
+    kv = B.KV8(1, 16, heads, d, i32([[0], [0], [0]]))
+    pos = [2] * 64 + [5] * 65 + [8 + i % 4 for i in range(200)]
+    cu = i32([0, 64, 129, 329])
+    x = torch.randn(m, heads, d, generator=torch.Generator().manual_seed(6))
+    B.sl_kv8_write(kv, x.to(DEV), (-x).to(DEV), i32(pos), cu, m)
+    k, v = (torch.empty(m, heads, d, device=DEV) for _ in range(2))
+    B.sl_kv8_read(kv, k, v, i32(pos), cu, m)
+    # rows on slots 8 .. 11 in turn name a slot again four rows on; they share the quad and stay in order
+    last = {p: max(i for i in range(m) if pos[i] == p) for p in set(pos)}
+    want = torch.as_tensor(ref.kv8_values(ref.f64(x)))[[last[p] for p in pos]].float()
+    assert torch.equal(k.cpu(), want) and torch.equal(v.cpu(), -want)
+
+
 # ---- attention ----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("d", [32, 64, 128, 256])
 @pytest.mark.parametrize("dtype", [BF, F])
