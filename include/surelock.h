@@ -430,7 +430,7 @@ int sl_peak_probe_stream(void *stream, const void *src, void *dst, size_t bytes,
  *   scales [n, ceil(k/group)] bf16
  *   zeros  [n, ceil(k/group)] u8, 0..15 (upper halves are ignored); or null: 8 everywhere
  * and stands for W[j, i] = scales[j, i/group] * (code - zeros[j, i/group]).  group is 32, 64 or 128; n >= 1; k >= 8 and a
- * multiple of 8 (the last group may be short); n, k <= 2^24.
+ * multiple of 8 (the last group may be short); n, k <= 2^24, n k <= 2^36.
  *
  * sl_linear_q4_quantize: codes, scales and zeros of a plain W (dtype SL_F32 / SL_BF16), nearest code per group, all in fp32:
  * with zeros, lo = min(0, min w), hi = max(0, max w), scale = bf16((hi - lo) / 15), zero = rint(-lo / scale) in 0..15, code =
@@ -474,7 +474,7 @@ int sl_kv8_bytes(int32_t n_pages, int32_t page_slots, int32_t n_kv_heads, int32_
  *   k, v     [m_upper] rows of [n_kv_heads, d_head] (dtype SL_F32 / SL_BF16), k_stride / v_stride elements apart (a
  *            projection's fused output has such strides); 16-byte aligned, strides a multiple of 16 bytes
  *   cu_rows  [batch + 1] i32: rows cu_rows[b] .. cu_rows[b + 1] - 1 belong to sequence b (cu_active of a step is one such)
- *   row_pos  [m_upper] i32: the row's slot in its sequence
+ *   row_pos  [m_upper] i32: the row's slot in its sequence;  m_upper <= 2^20
  * Rows from cu_rows[batch] on are left alone.  A row whose slot is negative, past the table or on no page is not written;
  * read back it is zeros.  Of adjacent rows that name one slot the last is kept; rows that name one slot must be
  * adjacent.  Values read back are code * scale in fp32, rounded to dtype.  A page may be shared by sequences that read it;
@@ -486,7 +486,7 @@ int sl_kv8_read(void *stream, const sl_kv8 *kv /* host */, void *k, void *v, int
 /* Attention of each row over the slots of its sequence:
  *   out[r, h] = sum_p softmax_p(scale * q[r, h] . K[p, h / share]) V[p, h / share],  share = n_heads / n_kv_heads,
  * p over the first min(seq_len[b], row_len[r]) slots (no more than the table's and than len_upper), without those on no page.
- * A row that sees no slot gets zeros.
+ * A row that sees no slot gets zeros.  n_heads <= 2^14, m_upper <= 2^20, their product <= 2^27; scale positive and finite.
  *   q, out   [m_upper] rows of [n_heads, d_head] (dtype), q_stride / out_stride elements apart, aligned as above; out must not
  *            overlap q
  *   seq_len  [batch] i32;  row_len [m_upper] i32, or null: every row sees its whole sequence

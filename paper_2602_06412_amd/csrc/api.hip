@@ -703,7 +703,8 @@ extern "C" int sl_unlock_rule(sl_ctx* ctx, void* stream, uint8_t* lock, uint8_t*
 
 // ---- 4-bit weights -------------------------------------------------------------------------------------
 static bool q4_shape_ok(int32_t n, int32_t k, int32_t group) {
-  return n >= 1 && n <= 1 << 24 && k >= 8 && k <= 1 << 24 && k % 8 == 0 && (group == 32 || group == 64 || group == 128);
+  if (n < 1 || n > 1 << 24 || k < 8 || k > 1 << 24 || k % 8 || (int64_t)n * k > (int64_t)1 << 36) return false;
+  return group == 32 || group == 64 || group == 128;
 }
 
 extern "C" int sl_linear_q4_quantize(void* stream, const void* w, int32_t dtype, int32_t n, int32_t k, int32_t group, void* codes,
@@ -779,7 +780,7 @@ static bool kv8_rows_ok(const void* p, int64_t stride, int64_t width, int32_t dt
 static int kv8_check_rows(const sl_kv8* kv, const void* k, const void* v, int32_t dtype, int64_t k_stride, int64_t v_stride,
                           const int32_t* row_pos, const int32_t* cu_rows, int32_t m_upper) {
   SL_TRY(kv8_check(kv));
-  if (!row_pos || !cu_rows || m_upper < 0 || (dtype != SL_F32 && dtype != SL_BF16)) return SL_EINVAL;
+  if (!row_pos || !cu_rows || m_upper < 0 || m_upper > 1 << 20 || (dtype != SL_F32 && dtype != SL_BF16)) return SL_EINVAL;
   const int64_t width = (int64_t)kv->n_kv_heads * kv->d_head;
   return kv8_rows_ok(k, k_stride, width, dtype) && kv8_rows_ok(v, v_stride, width, dtype) ? SL_OK : SL_EINVAL;
 }
@@ -801,7 +802,7 @@ extern "C" int sl_kv8_read(void* stream, const sl_kv8* kv, void* k, void* v, int
 static int kv8_attention_shape(const sl_kv8* kv, int32_t n_heads, int32_t m_upper, int32_t len_upper) {
   SL_TRY(kv8_check(kv));
   if (n_heads < 1 || n_heads > 1 << 14 || n_heads % kv->n_kv_heads || m_upper < 0 || m_upper > 1 << 20 || len_upper < 0) return SL_EINVAL;
-  if ((int64_t)m_upper * n_heads > (int64_t)1 << 28) return SL_EINVAL;
+  if ((int64_t)m_upper * n_heads > (int64_t)1 << 27) return SL_EINVAL;
   return SL_OK;
 }
 

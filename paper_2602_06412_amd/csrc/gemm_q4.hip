@@ -286,7 +286,7 @@ int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int g
 
 int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
                   void* y_bf16, const int32_t* row_map) {
-  // Tiles, us by tile (rows x columns, waves side by side x along the reduction; "-" not measured with that one alone):
+  // Tiles, us by tile (rows x columns, waves side by side x along the reduction):
   //   n, k, rows            16x16,1x16  16x32,1x8  16x48,1x8  32x32,1x8  32x128,4x2
   //   4096, 4096, 1             6.5        7.7        8.4        9.5        18
   //   4096, 12288, 16          11.7       15.7       19.2       21.7        58
@@ -299,14 +299,14 @@ int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_
   // Few rows are a matter of the weights' latency: workgroups enough for all CUs, many waves along the reduction, and as many columns as
   // still leave one workgroup to a CU.  Many rows are a matter of unpacking weights and of moving rows: a large tile whose waves share
   // them, once there are enough of it.
-  const int rows16 = sl_cdiv(m_upper, 16), tiles_n = sl_cdiv(n, kCols), blocks_k = sl_cdiv(k, kDepth);
+  const int64_t rows16 = sl_cdiv(m_upper, 16), tiles_n = sl_cdiv(n, kCols), blocks_k = sl_cdiv(k, kDepth);
 #define Q4_RUN(GS, MT, CT, WN, WK, U)                                                                                                  \
   hipLaunchKernelGGL((q4_linear_kernel<GS, MT, CT, WN, WK, U>), dim3(sl_cdiv(n, kCols * CT * WN), sl_cdiv(m_upper, 16 * MT)),          \
                      dim3(64 * WN * WK), 0, s, (const bf16_t*)x, (const unsigned char*)packed, m_dev, m_upper, n, k, y_f32,             \
                      (bf16_t*)y_bf16, row_map)
 #define Q4_BY_TILE(GS)                                                                                                                 \
   do {                                                                                                                                 \
-    if (rows16 >= 3 && sl_cdiv(n, 128) * sl_cdiv(m_upper, 32) >= 192) Q4_RUN(GS, 2, 2, 4, 2, 2);                                       \
+    if (rows16 >= 3 && (int64_t)sl_cdiv(n, 128) * sl_cdiv(m_upper, 32) >= 192) Q4_RUN(GS, 2, 2, 4, 2, 2);                                       \
     else if (rows16 >= 3) Q4_RUN(GS, 2, 2, 1, 8, 1);                                                                                   \
     else if (rows16 == 1 && tiles_n <= 256 && blocks_k >= 16) Q4_RUN(GS, 1, 1, 1, 16, 1);                                              \
     else if (tiles_n * rows16 <= 512) Q4_RUN(GS, 1, 2, 1, 8, 1);                                                                       \

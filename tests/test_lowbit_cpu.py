@@ -22,7 +22,7 @@ QUANT = dict(stream=None, w=256, dtype=1, n=64, k=256, group=64, codes=256, scal
 
 
 @pytest.mark.parametrize("change", [dict(x=None), dict(packed=None), dict(m=None), dict(m_upper=-1), dict(m_upper=(1 << 20) + 1), dict(n=0),
-                                    dict(n=(1 << 24) + 1), dict(k=0), dict(k=260), dict(k=1 << 25), dict(group=16), dict(group=256),
+                                    dict(n=(1 << 24) + 1), dict(k=0), dict(k=260), dict(k=1 << 25), dict(n=1 << 20, k=1 << 20), dict(group=16), dict(group=256),
                                     dict(y_f32=None), dict(y_bf16=256), dict(row_map=256), dict(x=264), dict(packed=264), dict(y_f32=258)])
 def test_q4_forward_refuses(change):
     assert call("sl_linear_q4_forward", FORWARD) == OK                     # no rows: nothing to launch
@@ -72,7 +72,7 @@ def test_kv8_rows_refuse(name):
         assert call(name, good, kv=cache(**c)) == BAD, c
     assert call(name, good, kv=cache(pool_bytes=100)) == SMALL
     for c in (dict(kv=None), dict(k=None), dict(v=None), dict(k=264), dict(v=264), dict(dtype=2), dict(ks=511), dict(ks=516), dict(vs=508),
-              dict(pos=None), dict(cu=None), dict(m=-1), dict(vs=1 << 41)):
+              dict(pos=None), dict(cu=None), dict(m=-1), dict(m=(1 << 20) + 1), dict(vs=1 << 41)):
         assert call(name, good, **c) == BAD, c
 
 
@@ -82,7 +82,7 @@ def test_kv8_attention_refuses():
     for c in BAD_CACHE:
         assert call("sl_kv8_attention", good, kv=cache(**c)) == BAD, c
     for c in (dict(kv=None), dict(q=None), dict(out=None), dict(q=264), dict(out=264), dict(dtype=7), dict(qs=1023), dict(qs=1028), dict(outs=1016),
-              dict(heads=0), dict(heads=6), dict(heads=1 << 17), dict(cu=None), dict(len=None), dict(m=-1), dict(m=(1 << 20) + 1), dict(upper=-1),
+              dict(heads=0), dict(heads=6), dict(heads=1 << 15), dict(m=1 << 20, heads=256, qs=1 << 15, outs=1 << 15), dict(cu=None), dict(len=None), dict(m=-1), dict(m=(1 << 20) + 1), dict(upper=-1),
               dict(scale=C.c_float(0.0)), dict(scale=C.c_float(float("inf"))), dict(scale=C.c_float(float("nan"))), dict(ws=None), dict(ws=128)):
         assert call("sl_kv8_attention", good, **c) == BAD, c
     assert call("sl_kv8_attention", good, m=1, size=0) == SMALL            # refused before anything is launched
