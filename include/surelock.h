@@ -430,12 +430,12 @@ int sl_peak_probe_stream(void *stream, const void *src, void *dst, size_t bytes,
  *   scales [n, ceil(k/group)] bf16
  *   zeros  [n, ceil(k/group)] u8, 0..15 (upper halves are ignored); or null: 8 everywhere
  * and stands for W[j, i] = scales[j, i/group] * (code - zeros[j, i/group]).  group is 32, 64 or 128; n >= 1; k >= 8 and a
- * multiple of 8 (the last group may be short); n, k <= 2^24, n k <= 2^36.
+ * multiple of 8 (the last group may be short); n, k <= 2^24, n k <= 2^34.
  *
  * sl_linear_q4_quantize: codes, scales and zeros of a plain W (dtype SL_F32 / SL_BF16), nearest code per group, all in fp32:
  * with zeros, lo = min(0, min w), hi = max(0, max w), scale = bf16((hi - lo) / 15), zero = rint(-lo / scale) in 0..15, code =
  * rint(w / scale) + zero in 0..15; without, scale = bf16(max|w| / 7), code = rint(w / scale) + 8 in 0..15.  A group of zeros has
- * scale 0; one that holds a NaN or an infinity has scale NaN, and so has every weight of it.
+ * scale 0; one that holds a NaN or an infinity has scale NaN, and so has every weight of it.  w is 16-byte, codes 4-byte aligned.
  * sl_linear_q4_bytes / sl_linear_q4_pack: size of, and conversion into, the layout sl_linear_q4_forward reads (codes of a
  * matrix-core operand in one 16-byte load); packed is 16-byte aligned. */
 int sl_linear_q4_quantize(void *stream, const void *w, int32_t dtype, int32_t n, int32_t k, int32_t group, void *codes,
@@ -447,7 +447,8 @@ int sl_linear_q4_pack(void *stream, const void *codes, const void *scales, const
  * exactly one of
  *   y_f32  [m_upper, n] fp32, or
  *   y_bf16 [*, n] bf16, row r written to row row_map[r] (row_map may be null; only with y_bf16)
- * is non-null.  Rows past the count are neither read nor written.  No workspace; the same sums in the same order in every
+ * is non-null.  Rows past the count are neither read nor written.  A row that holds a NaN or an infinity, or whose largest
+ * sums exceed fp32's range / 15, comes out as NaN (its code and zero-point sums are taken apart).  No workspace; the same sums in the same order in every
  * call of one m_upper.  m_upper <= 2^20.  Made for few rows: weights are unpacked once per 64 rows at most, so that hundreds of rows
  * are a matter of the matrix units; thousands of rows are better served by sl_linear_forward. */
 int sl_linear_q4_forward(void *stream, const void *x, const void *packed, const int32_t *m_dev, int32_t m_upper,

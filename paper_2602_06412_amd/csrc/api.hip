@@ -703,7 +703,7 @@ extern "C" int sl_unlock_rule(sl_ctx* ctx, void* stream, uint8_t* lock, uint8_t*
 
 // ---- 4-bit weights -------------------------------------------------------------------------------------
 static bool q4_shape_ok(int32_t n, int32_t k, int32_t group) {
-  if (n < 1 || n > 1 << 24 || k < 8 || k > 1 << 24 || k % 8 || (int64_t)n * k > (int64_t)1 << 36) return false;
+  if (n < 1 || n > 1 << 24 || k < 8 || k > 1 << 24 || k % 8 || (int64_t)n * k > (int64_t)1 << 34) return false;
   return group == 32 || group == 64 || group == 128;
 }
 
@@ -711,7 +711,7 @@ extern "C" int sl_linear_q4_quantize(void* stream, const void* w, int32_t dtype,
                                      void* scales, void* zeros) {
   if (!w || !codes || !scales || !q4_shape_ok(n, k, group)) return SL_EINVAL;
   if (dtype != SL_F32 && dtype != SL_BF16) return SL_EINVAL;
-  if ((uintptr_t)w % sl_tsize(dtype) || (uintptr_t)scales % 2) return SL_EINVAL;
+  if ((uintptr_t)w % 16 || (uintptr_t)codes % 4 || (uintptr_t)scales % 2) return SL_EINVAL;
   return slk_q4_quantize((hipStream_t)stream, w, dtype, n, k, group, codes, scales, zeros);
 }
 

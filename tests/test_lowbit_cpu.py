@@ -37,7 +37,7 @@ def test_q4_pack_refuses(change):
     assert call("sl_linear_q4_pack", PACK, **change) == BAD
 
 
-@pytest.mark.parametrize("change", [dict(w=None), dict(codes=None), dict(scales=None), dict(dtype=2), dict(dtype=-1), dict(w=257), dict(k=20),
+@pytest.mark.parametrize("change", [dict(w=None), dict(codes=None), dict(scales=None), dict(dtype=2), dict(dtype=-1), dict(w=264), dict(codes=258), dict(scales=257), dict(k=20),
                                     dict(n=-1), dict(group=48)])
 def test_q4_quantize_refuses(change):
     assert call("sl_linear_q4_quantize", QUANT, **change) == BAD
