@@ -447,10 +447,10 @@ int sl_linear_q4_pack(void *stream, const void *codes, const void *scales, const
  * exactly one of
  *   y_f32  [m_upper, n] fp32, or
  *   y_bf16 [*, n] bf16, row r written to row row_map[r] (row_map may be null; only with y_bf16)
- * is non-null.  Rows past the count are neither read nor written.  A row that holds a NaN or an infinity, or whose largest
- * sums exceed fp32's range / 15, comes out as NaN (its code and zero-point sums are taken apart).  No workspace; the same sums in the same order in every
- * call of one m_upper.  m_upper <= 2^20.  Made for few rows: weights are unpacked once per 64 rows at most, so that hundreds of rows
- * are a matter of the matrix units; thousands of rows are better served by sl_linear_forward. */
+ * is non-null.  Rows past the count are neither read nor written.  A row that holds a NaN or an infinity, or whose sums leave
+ * fp32's range when multiplied by 15, comes out as NaN (sums over codes and over zero points are taken apart).  No workspace;
+ * the same sums in the same order in every call of one m_upper.  m_upper <= 2^20.  Made for few rows: weights are unpacked
+ * again for every 32 rows, so hundreds of rows are a matter of that, and thousands better served by sl_linear_forward. */
 int sl_linear_q4_forward(void *stream, const void *x, const void *packed, const int32_t *m_dev, int32_t m_upper,
                          int32_t n, int32_t k, int32_t group, float *y_f32, void *y_bf16, const int32_t *row_map);
 

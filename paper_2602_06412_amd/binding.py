@@ -401,6 +401,8 @@ def sl_linear_q4_pack(codes, scales, zeros, n, k, group, packed):
 
 def sl_linear_q4_forward(x, packed, m_dev, m_upper, n, k, group, y_f32=None, y_bf16=None, row_map=None):
     _require_gpu(x)
+    if m_upper == 0:                       # (empty tensors have no address)
+        return
     dev, stream = _here()
     status = lib().sl_linear_q4_forward(stream, _addr(x, _BF16, dev), _addr(packed, _U8, dev), _addr(m_dev, _I32, dev), m_upper, n, k, group,
                                         _addr(y_f32, _F32, dev), _addr(y_bf16, _BF16, dev), _addr(row_map, _I32, dev))
@@ -443,6 +445,8 @@ def _head_rows(t, dtype, dev, heads, d):
 
 def _kv8_rows(name, fn, kv, k, v, row_pos, cu_rows, m_upper):
     _require_gpu(k)
+    if m_upper == 0:
+        return
     dev, stream = _here()
     dtype, heads, d = k.dtype, kv.n_kv_heads, kv.d_head
     (kp, ks), (vp, vs) = _head_rows(k, dtype, dev, heads, d), _head_rows(v, dtype, dev, heads, d)
@@ -468,6 +472,8 @@ def sl_kv8_attention_bytes(kv, n_heads, m_upper, len_upper):
 def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, workspace, row_len=None):
     """q, out: rows [*, n_heads, d_head]."""
     _require_gpu(q)
+    if m_upper == 0:
+        return
     dev, stream = _here()
     dtype, n_heads, d = q.dtype, q.shape[1], kv.d_head
     (qp, qs), (op, os_) = _head_rows(q, dtype, dev, n_heads, d), _head_rows(out, dtype, dev, n_heads, d)

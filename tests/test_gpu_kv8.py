@@ -365,6 +365,34 @@ def test_same_bits_whatever_the_workspace_holds_and_on_another_stream():
     assert np.array_equal(a, b) and np.array_equal(a, s)
 
 
+def test_what_the_binding_refuses_and_what_is_nothing_to_do():
+    """Types, layouts and devices that the library would misread raise; no rows at all are fine."""
+    c = Case([20], 2, 64, 16, BF, seed=19)
+    q = torch.zeros(1, 2, 64, dtype=BF, device=DEV)
+    ws = torch.empty(256, dtype=torch.uint8, device=DEV)
+    good = dict(kv=c.kv, q=q, cu_rows=i32([0, 1]), seq_len=i32([20]), m_upper=1, len_upper=20, scale=0.1, out=torch.zeros_like(q), workspace=ws)
+    B.sl_kv8_attention(**good)
+    for change in (dict(q=q.cpu()), dict(q=q.half()), dict(q=q.float()), dict(out=q[0]), dict(seq_len=torch.tensor([20], device=DEV)),
+                   dict(cu_rows=torch.tensor([0, 1], dtype=torch.int32)), dict(q=torch.zeros(1, 64, 2, dtype=BF, device=DEV).transpose(1, 2)),
+                   dict(workspace=ws.float()), dict(row_len=torch.zeros(1, device=DEV))):
+        with pytest.raises((ValueError, KeyError)):
+            B.sl_kv8_attention(**dict(good, **change))
+    with pytest.raises(B.SureLockError) as e:
+        B.sl_kv8_attention(**dict(good, len_upper=100000, workspace=ws[:0]))
+    assert e.value.status in (B.SL_EINVAL, B.SL_ENOSPC)
+    none = torch.zeros(0, 2, 64, dtype=BF, device=DEV)
+    B.sl_kv8_attention(**dict(good, q=none, out=none, m_upper=0))
+    B.sl_kv8_write(c.kv, none, none, i32([0]), i32([0, 0]), 0)
+    x = torch.zeros(2, 64, dtype=BF, device=DEV)
+    packed = torch.empty(B.sl_linear_q4_bytes(8, 64, 32), dtype=torch.uint8, device=DEV)
+    for change in (dict(x=x.float()), dict(x=x.cpu()), dict(x=torch.zeros(64, 2, dtype=BF, device=DEV).T), dict(y_f32=torch.zeros(2, 8, dtype=BF, device=DEV)),
+                   dict(m_dev=torch.tensor([2], device=DEV)), dict(packed=packed.float())):
+        args = dict(dict(x=x, packed=packed, m_dev=i32([2]), m_upper=2, n=8, k=64, group=32, y_f32=torch.zeros(2, 8, device=DEV)), **change)
+        with pytest.raises(ValueError):
+            B.sl_linear_q4_forward(**args)
+    B.sl_linear_q4_forward(x[:0], packed, i32([0]), 0, 8, 64, 32, y_f32=torch.zeros(0, 8, device=DEV))
+
+
 # ---- a decoding block's few-row work, all together ----------------------------------------------------------
 def _block(st):
     """Q|K|V with 4-bit weights, the rows' K and V into the cache, attention, Out with 4-bit weights."""
