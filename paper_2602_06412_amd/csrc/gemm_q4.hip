@@ -66,7 +66,7 @@ __device__ inline float over_lanes(float v, F f) {
 }
 
 // Range, scale, zero point and codes; eight numbers a lane, group / 8 lanes a group.  24576 x 4096 bf16 take 92 us (253 MB, 2.8 TB/s:
-// the quotients' divisions bound it; it runs once, when weights are loaded); a thread for each group took 3.7 ms.
+// the quotients' divisions are taken to bound it; it runs once, when weights are loaded); a thread for each group took 3.7 ms.
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void q4_quantize_kernel(const T* w, int n, int k, int groups, unsigned char* codes, bf16_t* scales, unsigned char* zeros) {
   constexpr int L = GROUP / 8;
@@ -134,7 +134,7 @@ __device__ inline float sum_of_piece(const uint4& v) {
 //
 // Rows pass through LDS, once for the WN waves of a group, and with them goes the sum of each group of weights' inputs.  An
 // operand has 16 rows side by side in a wave's lanes, and loaded so from row-major memory every lane is an access of its own (16
-// bytes a cycle of the address unit, which was busy 70 to 88 % of the time: 61 rows, n = 4096, k = 12288 took 53 us for 33).  Here eight
+// bytes a cycle of the address unit, which was busy 70 % of the time: 61 rows, n = 4096, k = 12288 took 53 us for 33).  Here eight
 // lanes take a row's 128 consecutive bytes; 16-byte pieces that would meet in one bank are kept apart by an exclusive or of their row
 // with their place.
 template <int GS, int MT, int CT, int WN, int WK, int U>
