@@ -417,11 +417,15 @@ class KV8:
 
     def __init__(self, n_pages, page_slots, n_kv_heads, d_head, page_table, pool=None):
         need = sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head)
+        _require_gpu(page_table)
+        self.device = page_table.get_device()
+        if pool is not None and pool.device != page_table.device:
+            raise ValueError(f"the pool is on {pool.device}, its page table on {page_table.device}")
         self.pool = torch.empty(need, dtype=torch.uint8, device=page_table.device) if pool is None else pool
         self.page_table, self.n_kv_heads, self.d_head = page_table, n_kv_heads, d_head
         batch, max_pages = page_table.shape
-        _require_gpu(page_table)
-        self.desc = sl_kv8(_ptr(self.pool), _nbytes(self.pool), _addr(page_table, _I32, page_table.get_device()), n_pages, page_slots, n_kv_heads, d_head, batch, max_pages)
+        self.desc = sl_kv8(_ptr(self.pool), _nbytes(self.pool), _addr(page_table, _I32, self.device), n_pages, page_slots,
+                           n_kv_heads, d_head, batch, max_pages)
         self.desc_ref = C.byref(self.desc)
 
     def sequence(self, b):
@@ -432,6 +436,14 @@ def sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head):
     out = _Z()
     _check("sl_kv8_bytes", lib().sl_kv8_bytes(n_pages, page_slots, n_kv_heads, d_head, C.byref(out)))
     return out.value
+
+
+def _kv8_here(kv):
+    """As _here, for a cache on the current device."""
+    dev, stream = _here()
+    if kv.device != dev:
+        raise ValueError(f"the cache is on cuda:{kv.device}, the current device is cuda:{dev}")
+    return dev, stream
 
 
 def _head_rows(t, dtype, dev, heads, d):
@@ -447,7 +459,7 @@ def _kv8_rows(name, fn, kv, k, v, row_pos, cu_rows, m_upper):
     _require_gpu(k)
     if m_upper == 0:
         return
-    dev, stream = _here()
+    dev, stream = _kv8_here(kv)
     dtype, heads, d = k.dtype, kv.n_kv_heads, kv.d_head
     (kp, ks), (vp, vs) = _head_rows(k, dtype, dev, heads, d), _head_rows(v, dtype, dev, heads, d)
     status = fn(stream, kv.desc_ref, kp, vp, _DTYPE_CODES[dtype], ks, vs, _addr(row_pos, _I32, dev), _addr(cu_rows, _I32, dev), m_upper)
@@ -474,7 +486,7 @@ def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, wo
     _require_gpu(q)
     if m_upper == 0:
         return
-    dev, stream = _here()
+    dev, stream = _kv8_here(kv)
     dtype, n_heads, d = q.dtype, q.shape[1], kv.d_head
     (qp, qs), (op, os_) = _head_rows(q, dtype, dev, n_heads, d), _head_rows(out, dtype, dev, n_heads, d)
     status = lib().sl_kv8_attention(stream, kv.desc_ref, qp, _DTYPE_CODES[dtype], qs, n_heads, _addr(cu_rows, _I32, dev),

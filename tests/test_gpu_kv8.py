@@ -393,6 +393,23 @@ def test_what_the_binding_refuses_and_what_is_nothing_to_do():
     B.sl_linear_q4_forward(x[:0], packed, i32([0]), 0, 8, 64, 32, y_f32=torch.zeros(0, 8, device=DEV))
 
 
+def test_a_cache_on_another_device_is_refused():
+    """The kernels would follow its pool and page table: no call starts unless both are on the current device."""
+    c = Case([20], 2, 64, 16, BF, seed=23)
+    with pytest.raises(ValueError):
+        B.KV8(c.n_pages, 16, 2, 64, i32(c.table), c.kv.pool.cpu())
+    with pytest.raises(ValueError):
+        B.KV8(c.n_pages, 16, 2, 64, i32(c.table).cpu())
+    x = torch.zeros(1, 2, 64, dtype=BF, device=DEV)
+    away = c.kv.sequence(0)
+    away.device += 1                                        # as a cache of another device says
+    for call in (lambda: B.sl_kv8_write(away, x, x, i32([0]), i32([0, 1]), 1), lambda: B.sl_kv8_read(away, x, x, i32([0]), i32([0, 1]), 1),
+                 lambda: B.sl_kv8_attention(away, x, i32([0, 1]), i32([20]), 1, 20, 0.1, torch.zeros_like(x),
+                                            torch.empty(256, dtype=torch.uint8, device=DEV))):
+        with pytest.raises(ValueError):
+            call()
+
+
 # ---- a decoding block's few-row work, all together ----------------------------------------------------------
 def _block(st):
     """Q|K|V with 4-bit weights, the rows' K and V into the cache, attention, Out with 4-bit weights."""
