@@ -15,7 +15,8 @@
 //   V becomes half precision in two operations a pair: 0x6400 + (code + 128) are the bits of the half 1024 + code + 128.
 //   A probability times V's scale goes in as two halves (22 bits), scaled by a power of two per query so that the largest seen lies
 //     below 2^14: what is 2^38 times smaller than it is dropped.  One half would leave 11 bits, against a result rounded to 8 in
-//     bf16, but to 24 in fp32.
+//     bf16, but to 24 in fp32.  "The largest" is what is left of it: as the maximum rises, weights seen before shrink, and the power
+//     of two follows (kept from them as they were, it dropped a slot that held all the weight where earlier values were 10^12 larger).
 // Scores, maximum, sum and output accumulate in fp32.
 #include "kv8.h"
 
@@ -267,6 +268,7 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
   f32x4 o[DT] = {};
   float m = kNegInf, l = 0.f;                             // of this wave's slots; l of this lane's
   int top = -300;                                         // o is scaled by 2^(kTop - top)
+  float peak = kNegInf;                                   // binary exponent of the largest weight so far, before a maximum is taken off
   for (int step = 0; s0 < end; ++step) {
     const int here = s0, ok_here = ok;
     const bool whole = here + kStep <= least && ok == (1 << ST) - 1;      // every query sees every slot of the step
@@ -316,7 +318,11 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
         most_w = fmaxf(most_w, s[j][i]);
       }
     most_w = max_across(most_w);
-    const int top_new = max(top, most_w > 0.f ? __builtin_amdgcn_frexp_expf(most_w) : -300);
+    // weights below 2^now are added in this step, what is left of earlier ones lies below 2^(peak - base); scores far beyond fp32's
+    // integers may miss the latter, which costs bits and no more: o's own scale is whatever top is
+    const int now = most_w > 0.f ? __builtin_amdgcn_frexp_expf(most_w) : -300;
+    peak = fmaxf(peak, most_w > 0.f ? base + (float)now : kNegInf);
+    const int top_new = max(now, (int)fmaxf(ceilf(peak - base), -300.f));
     const float alpha = __builtin_amdgcn_exp2f(m - base);
     l = fmaf(l, alpha, sum);
     if (__any(top_new != top || m_new != m)) {

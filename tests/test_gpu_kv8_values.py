@@ -1,0 +1,96 @@
+"""sl_kv8_attention on values and queries of very different size, against its definition in 64 bits.
+
+The bound (`bound`) goes by what an error does to the result.  With e = 2^-24 and weights P:
+  a score s = scale q . k in fp32: at most 3 d + 16 roundings of its sum of absolute terms (`size`), and the distance to a maximum and
+  between maxima 8 more; scores off by at most D each move the result by at most D sum P |v - o| to first order (`spread`), 1.2 of that while
+  D < 0.1 -- a sharp softmax forgives what a dot product loses;
+  sums over slots, exponentials, the join: slots + 64 roundings of sum P |v| (`mass`);
+  bf16: a weight goes in with 22 bits, or to 2^-39 of the row's largest weight times its vector's largest number (`peak`), whichever is coarser;
+  probabilities below 2^-126 are zero;
+  half a step of the result's type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_06412_amd import binding as B
+from tests import lowbit_ref as ref
+from tests.gpu_util import DEV
+from tests.test_gpu_kv8 import Case, i32
+
+pytestmark = pytest.mark.gpu
+BF, F = torch.bfloat16, torch.float32
+E = 2.0 ** -24
+
+
+def attention(q, K, V, scale, dtype):
+    """q [d], K, V [slots, d], float64 -> (o, bound)."""
+    n, d = K.shape
+    s = scale * (K @ q)
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    o, mass = p @ V, p @ np.abs(V)
+    D = (3 * d + 24) * E * scale * np.max(np.abs(K) @ np.abs(q))
+    assert D < 0.1
+    err = 1.2 * D * (p @ np.abs(V - o)) + (n + 64) * E * mass + n * 2.0 ** -126 * np.abs(V).max()
+    if dtype is BF:
+        err = err + 2.0 ** -22 * mass + n * 2.0 ** -39 * (p * np.abs(V).max(1)).max()
+    return o, err + np.abs(o) * torch.finfo(dtype).eps / 2 * 1.01 + 2.0 ** -149
+
+
+def filled(k, v, page=64):
+    """A cache of sequences k[b], v[b] [slots, heads, d]."""
+    c = Case([len(x) for x in k], k[0].shape[1], k[0].shape[2], page, k[0].dtype)
+    c.k, c.v = list(k), list(v)
+    c.write([list(range(len(x))) for x in k])
+    c.K, c.V = [ref.kv8_values(ref.f64(x)) for x in k], [ref.kv8_values(ref.f64(x)) for x in v]
+    return c
+
+
+def check(c, q, got, rows):
+    """rows: the sequence of each row; every row sees its whole sequence."""
+    share = q.shape[1] // c.heads
+    for r, b in enumerate(rows):
+        for h in range(q.shape[1]):
+            want, bound = attention(ref.f64(q[r, h]), c.K[b][:, h // share], c.V[b][:, h // share], 1.0 / math.sqrt(c.d), c.dtype)
+            err = np.abs(got[r, h] - want)
+            assert (err <= bound).all(), (b, r, h, float(np.nanmax(err / bound)), float(np.abs(want).max()))
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed))
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("large", [1e4, 1e8, 1e12, 1e20])
+@pytest.mark.parametrize("at", [5, 300, 399])
+def test_small_values_that_take_the_weight_from_large_ones(dtype, large, at):
+    """One slot far ahead of the others (2^90 in weight), its value ordinary, the others' large: read before, between and after them."""
+    d, n = 64, 400
+    k, v = 0.01 * randn(1, n, 1, d), large * randn(2, n, 1, d)
+    k[at] = 0
+    k[at, :, 0] = 90 * math.log(2) * math.sqrt(d)
+    v[at] = randn(3, 1, d)
+    c = filled([k.to(dtype)], [v.to(dtype)])
+    q = torch.zeros(1, 1, d)
+    q[..., 0] = 1
+    q, got = c.attend([1], 1, q=q.to(dtype))
+    check(c, q, got, [0])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("falling", [False, True])
+def test_weights_that_rise_step_by_step(dtype, falling):
+    """Scores that rise by 5 (in powers of two) from one group of 128 slots to the next, values that fall by 2^10: each group takes the result over."""
+    d, n = 64, 512
+    group = torch.arange(n) // 128
+    k, v = torch.zeros(n, 1, d), randn(4, n, 1, d) * 2.0 ** (-10.0 * group)[:, None, None]
+    k[:, 0, 0] = 5 * math.log(2) * math.sqrt(d) * group
+    if falling:
+        k, v = k.flip(0).contiguous(), v.flip(0).contiguous()
+    c = filled([k.to(dtype)], [v.to(dtype)])
+    q = torch.zeros(1, 1, d)
+    q[..., 0] = 1
+    q, got = c.attend([1], 1, q=q.to(dtype))
+    check(c, q, got, [0])
