@@ -32,31 +32,26 @@ constexpr float kMagic = 12582912.f;                      // its float
 constexpr int kTop = 14;                                  // probabilities lie below 2^kTop
 
 // a lane's share of an 8-bit operand: 16 bytes (8 with d = 32)
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int E> struct Piece;
 template <> struct Piece<8> {
-  typedef uint2 type;
-  static __device__ i32x4 mfma(const uint2& a, const uint2& b, i32x4 c) {
+  typedef u32x2 type;
+  static __device__ i32x4 mfma(u32x2 a, u32x2 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
   }
 };
 template <> struct Piece<16> {
-  typedef uint4 type;
-  static __device__ i32x4 mfma(const uint4& a, const uint4& b, i32x4 c) {
+  typedef u32x4 type;
+  static __device__ i32x4 mfma(u32x4 a, u32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
 // (loads of codes that no other workgroup asks for go past the caches' replacement: the loads alone, of 830 MB, 133 us instead of 153)
 template <bool ONCE, typename P>
 __device__ inline P ask(const P* p) {
-  typedef uint32_t words __attribute__((ext_vector_type(sizeof(P) / 4)));
-  if constexpr (!ONCE) return *p;
-  const words w = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
-  P r;
-  __builtin_memcpy(&r, &w, sizeof(P));
-  return r;
+  return ONCE ? __builtin_nontemporal_load(p) : *p;
 }
-template <typename P>
-__device__ inline uint32_t word(const P& p, int i) { return reinterpret_cast<const uint32_t*>(&p)[i]; }
 
 // the other lanes' value, 16 / 32 lanes away, taken into a maximum or a sum without going through LDS
 template <typename F>
@@ -210,7 +205,7 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
   const int f = first + col;
   const bool live = f < queries;
   constexpr int QW = E * sizeof(T) / 16;                  // 16-byte words of this lane's share of a chunk
-  uint4 x[CH][QW];
+  u32x4 x[CH][QW];
   int limit = 0;
   {
     const int r = row0 + (live ? f / a.share : 0), h = kvh * a.share + (live ? f % a.share : 0);
@@ -219,11 +214,11 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int u = 0; u < QW; ++u) x[c][u] = reinterpret_cast<const uint4*>(qr + c * 4 * E + grp * E)[u];
+      for (int u = 0; u < QW; ++u) x[c][u] = reinterpret_cast<const u32x4*>(qr + c * 4 * E + grp * E)[u];
   }
   auto x_at = [&](int c, int u) {                         // number u of chunk c
-    if constexpr (sizeof(T) == 2) return __uint_as_float(u % 2 ? word(x[c][u / 8], u / 2 % 4) & 0xffff0000u : word(x[c][u / 8], u / 2 % 4) << 16);
-    else return __uint_as_float(word(x[c][u / 4], u % 4));
+    if constexpr (sizeof(T) == 2) return __uint_as_float(u % 2 ? x[c][u / 8][u / 2 % 4] & 0xffff0000u : x[c][u / 8][u / 2 % 4] << 16);
+    else return __uint_as_float(x[c][u / 4][u % 4]);
   };
   ask_k(s0, 0);                                           // (a wave without a step of its own asks for page 0: no branch)
   ask_v();
@@ -345,7 +340,7 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
       for (int c = 0; c < CH; ++c) {
 #pragma unroll
         for (int u = 0; u < E / 4; u += 2) {
-          const f16x8 v0 = v_halves(word(vc[j][c], u), word(vc[j + 1][c], u)), v1 = v_halves(word(vc[j][c], u + 1), word(vc[j + 1][c], u + 1));
+          const f16x8 v0 = v_halves(vc[j][c][u], vc[j + 1][c][u]), v1 = v_halves(vc[j][c][u + 1], vc[j + 1][c][u + 1]);
           f32x4 &o0 = o[c * (E / 4) + u], &o1 = o[c * (E / 4) + u + 1];
           o0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, hi, o0, 0, 0, 0);
           o1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, hi, o1, 0, 0, 0);
