@@ -494,8 +494,10 @@ int sl_kv8_read(void *stream, const sl_kv8 *kv /* host */, void *k, void *v, int
  *   len_upper      host: an upper bound on the slots any row sees; launches and workspace are sized by it
  *   workspace      sl_kv8_attention_bytes bytes, 256-byte aligned; needs no initialisation, two calls that may overlap in time
  *                  must not share one
- * Rows from cu_rows[batch] on are left as they are.  Scores, softmax statistics and sums are fp32; the same sums in the same
- * order in every call of the same bounds (no atomics). */
+ * Rows from cu_rows[batch] on are left as they are.  Scores, softmax statistics and sums are fp32.  fp32 queries and weights
+ * (probability times V's scale) keep 24 bits each; of bf16 queries, numbers below 2^-15 of their head's largest lose the bits
+ * under 2^-23 of it, and bf16 weights have 22 bits or, if coarser, 2^-39 of the row's largest.  The same sums in the same order in
+ * every call of the same bounds (no atomics). */
 int sl_kv8_attention_bytes(const sl_kv8 *kv /* host */, int32_t n_heads, int32_t m_upper, int32_t len_upper, size_t *out);
 int sl_kv8_attention(void *stream, const sl_kv8 *kv /* host */, const void *q, int32_t dtype, int64_t q_stride, int32_t n_heads,
                      const int32_t *cu_rows, const int32_t *seq_len, const int32_t *row_len, int32_t m_upper,

@@ -7,23 +7,29 @@
 // and slots 4 (l / 16) .. + 3 of a tile, which is the operand the second product wants, so probabilities never leave registers.
 //
 // Unpacking codes is what such a kernel would spend its instructions on: with K and V converted to bf16, 1.5 a number, the largest
-// case took 291 us, 180 as follows (its loads alone 170 at that stage):
+// case took 291 us, 180 as follows (its loads alone 170 at that stage).  For bf16 queries and results:
 //   K is not unpacked: the product is one of 8-bit integers, the query being a fixed-point number of three signed bytes,
-//     q = 2^(e - 22) (65536 a + 256 b + c), 2^(e-1) <= max|q| < 2^e: 23 bits of the row's largest number, as good as fp32's own sums.
+//     q = 2^(e - 22) (65536 a + 256 b + c), 2^(e-1) <= max|q| < 2^e.  Of 8 significant bits none is lost down to 2^-15 of the head's
+//     largest number; what lies below loses the bits under 2^-23 of it.
 //     Each byte's product starts from the integer 0x4B400000, whose bits are the float 1.5 * 2^23, so that the result, below 2^22
 //     for 256 dimensions, is that float plus itself: one subtraction instead of a conversion.
 //   V becomes half precision in two operations a pair: 0x6400 + (code + 128) are the bits of the half 1024 + code + 128.
 //   A probability times V's scale goes in as two halves (22 bits), scaled by a power of two per query so that the largest seen lies
-//     below 2^14: what is 2^38 times smaller than it is dropped.  One half would leave 11 bits, against a result rounded to 8 in
-//     bf16, but to 24 in fp32.  "The largest" is what is left of it: as the maximum rises, weights seen before shrink, and the power
-//     of two follows (kept from them as they were, it dropped a slot that held all the weight where earlier values were 10^12 larger).
+//     below 2^14: what is 2^38 times smaller than it is dropped.  One half would leave 11 bits, against a result rounded to 8.
+//     "The largest" is what is left of it: as the maximum rises, weights seen before shrink, and the power of two follows
+//     (kept from them as they were, it dropped a slot that held all the weight where earlier values were 10^12 larger).
+// For fp32 neither will do: a query's small numbers beside a large one, and a slot's small share of a dimension where the largest
+// slot holds nothing, have 24 bits of their own.  There K and V are converted to bf16, exactly, and a query's number and a weight go in
+// as three bf16 each, which hold all 24 bits at any size; products are exact, sums fp32.
 // Scores, maximum, sum and output accumulate in fp32.
 #include "kv8.h"
+#include <type_traits>
 
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr float kNegInf = -__builtin_inff();
@@ -72,6 +78,25 @@ __device__ inline f16x8 v_halves(uint32_t a, uint32_t b) {
   const f16x2 r2 = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u)) - off;
   const f16x2 r3 = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u)) - off;
   return f16x8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
+}
+
+// eight codes, signed bytes, as bf16
+__device__ inline bf16x8 codes_bf16(uint32_t a, uint32_t b) {
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = (__bf16)(float)(signed char)(a >> (8 * i));
+    r[4 + i] = (__bf16)(float)(signed char)(b >> (8 * i));
+  }
+  return r;
+}
+
+// a number as three bf16, all of its 24 bits
+__device__ inline void three_bf16(float x, __bf16& h, __bf16& m, __bf16& l) {
+  h = (__bf16)x;
+  const float r = x - (float)h;
+  m = (__bf16)r;
+  l = (__bf16)(r - (float)m);
 }
 
 // Four numbers of at most 2^22 in magnitude as three signed bytes each, base 256: byte p of all four in w[p].  A number plus
@@ -153,11 +178,15 @@ template <typename T, int D, bool ONCE>
 struct Kv8Segment {
   using Tile = Kv8Tile<D>;
   static constexpr int E = Tile::E, CH = Tile::CH, DT = D / 16;
+  static constexpr bool kFull = sizeof(T) == 4;           // all 24 bits of queries and weights
   typedef typename Piece<E>::type piece;
-  struct Shared {
-    float o[kWaves][16][D + 4];
+  typedef float Sums[kWaves][16][D + 4];
+  typedef uint32_t Bytes[CH][3][64][E / 4];               // the queries' bytes
+  typedef uint32_t Parts[CH][E / 8][3][64][4];            // the queries' bf16, eight a lane
+  struct Apart { Sums o; __attribute__((aligned(16))) Bytes q; };
+  struct OneAfterTheOther { union { Sums o; __attribute__((aligned(16))) Parts q; }; };
+  struct Shared : std::conditional<kFull, OneAfterTheOther, Apart>::type {
     float m[kWaves][16], l[kWaves][16];
-    __attribute__((aligned(16))) uint32_t q[CH][3][64][E / 4];       // the queries' bytes
   };
   static __device__ __forceinline__ void run(const Kv8View& kv, const Kv8Attn& a, Shared& sh, int b, const Kv8Sequence& seq, int kvh, int first,
                                              int from, int end, int part);
@@ -233,19 +262,39 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
   }));
   const bool finite = big < 0x7f800000u;
   const int qe = finite ? __builtin_amdgcn_frexp_expf(__uint_as_float(big)) : 0;
+  if constexpr (kFull) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int u = 0; u < E; u += 4)
-      if ((c * E + u) / 4 % kWaves == wave) {
-        float y[4];
-        uint32_t w[3];
+      for (int u = 0; u < E; u += 8)
+        if ((c * E + u) / 8 % kWaves == wave) {
+          bf16x8 w[3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_ldexpf(x_at(c, u + i), 22 - qe);
-        signed_bytes(y, w);
+          for (int i = 0; i < 8; ++i) {
+            __bf16 h, mid, low;
+            three_bf16(__builtin_amdgcn_ldexpf(x_at(c, u + i), 22 - qe), h, mid, low);
+            w[0][i] = h;
+            w[1][i] = mid;
+            w[2][i] = low;
+          }
 #pragma unroll
-        for (int p = 0; p < 3; ++p) sh.q[c][p][lane][u / 4] = w[p];
-      }
+          for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(sh.q[c][u / 8][p][lane]) = w[p];
+        }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int u = 0; u < E; u += 4)
+        if ((c * E + u) / 4 % kWaves == wave) {
+          float y[4];
+          uint32_t w[3];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_ldexpf(x_at(c, u + i), 22 - qe);
+          signed_bytes(y, w);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) sh.q[c][p][lane][u / 4] = w[p];
+        }
+  }
   // scores come out in powers of two: 2^(qe - 22), scale and log2(e) in one factor; NaN for a query that is not finite
   const float unit = finite ? __builtin_amdgcn_ldexpf(a.scale_log2, qe - 22) : __builtin_nanf("");
   const float unit_a = unit * 65536.f, unit_b = unit * 256.f, unit_c = -kMagic * unit;
@@ -269,6 +318,28 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
     const bool whole = here + kStep <= least && ok == (1 << ST) - 1;      // every query sees every slot of the step
     s0 += kWaves * kStep;
     float s[ST][4];
+    if constexpr (kFull) {
+      f32x4 acc[ST][3] = {};
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int u = 0; u < E / 8; ++u) {
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 k[ST];
+#pragma unroll
+          for (int j = 0; j < ST; ++j) k[j] = codes_bf16(kc[j][c][2 * u], kc[j][c][2 * u + 1]);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            const bf16x8 x = *reinterpret_cast<const bf16x8*>(sh.q[c][u][p][lane]);
+#pragma unroll
+            for (int j = 0; j < ST; ++j) acc[j][p] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], x, acc[j][p], 0, 0, 0);
+          }
+        }
+#pragma unroll
+      for (int j = 0; j < ST; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[j][i] = ks[j][i] * unit * (acc[j][0][i] + (acc[j][1][i] + acc[j][2][i]));
+    } else
 #pragma unroll
     for (int j = 0; j < ST; ++j) {
       const i32x4 zero = {kMagicBits, kMagicBits, kMagicBits, kMagicBits};
@@ -327,6 +398,26 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
     }
     m = m_new;
     top = top_new;
+    if constexpr (kFull) {
+      bf16x8 w[3];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __bf16 h, mid, low;
+        three_bf16(__builtin_amdgcn_ldexpf(s[i / 4][i % 4], kTop - top), h, mid, low);
+        w[0][i] = h;
+        w[1][i] = mid;
+        w[2][i] = low;
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int u = 0; u < E / 4; ++u) {
+          const bf16x8 v = codes_bf16(vc[0][c][u] ^ 0x80808080u, vc[1][c][u] ^ 0x80808080u);
+          f32x4& ou = o[c * (E / 4) + u];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) ou = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[p], ou, 0, 0, 0);
+        }
+    } else
 #pragma unroll
     for (int j = 0; j < ST; j += 2) {
       f16x8 hi, lo;
@@ -356,6 +447,7 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
   int tid = threadIdx.x, share = a.share;
   asm volatile("" : "+v"(tid), "+s"(share));
   l = sum_across(l);
+  if constexpr (kFull) __syncthreads();                   // the sums lie where the queries were
   const int lane_e = tid & 63, col_e = lane_e & 15, grp_e = lane_e >> 4;
   if (grp_e == 0) { sh.m[wave][col_e] = m; sh.l[wave][col_e] = l; }
 #pragma unroll

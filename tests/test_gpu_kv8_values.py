@@ -94,3 +94,38 @@ def test_weights_that_rise_step_by_step(dtype, falling):
     q[..., 0] = 1
     q, got = c.attend([1], 1, q=q.to(dtype))
     check(c, q, got, [0])
+
+
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("outlier", [1.0, 1e4, 1e6, 1e12])
+def test_fp32_queries_with_one_number_far_above_the_others(d, outlier):
+    """The keys hold nothing in that dimension (or little), so the scores are the others'.  fp32 keeps each number's own 24 bits."""
+    n, heads, share = 700, 2, 3
+    k, v, q = randn(5, n, heads, d), randn(6, n, heads, d), randn(7, 2, heads * share, d)
+    k[:, :, 5] = 0
+    q[..., 5] = outlier * (1 + torch.arange(2 * heads * share).view(2, -1) / 8)
+    c = filled([k], [v])
+    q, got = c.attend([2], share, q=q)
+    check(c, q, got, [0, 0])
+
+
+def test_bf16_queries_with_one_number_far_above_the_others():
+    """Up to 2^15 times the others' size nothing of theirs is lost."""
+    d, n = 128, 300
+    k, v, q = randn(5, n, 1, d).to(BF), randn(6, n, 1, d).to(BF), (randn(7, 2, 1, d).sign() * (1 + randn(8, 2, 1, d).abs() / 8)).to(BF)
+    k[:, :, 5] = 0
+    q[..., 5] = 2.0 ** 14
+    c = filled([k], [v])
+    q, got = c.attend([2], 1, q=q)
+    check(c, q, got, [0, 0])
+
+
+@pytest.mark.parametrize("outlier", [1e4, 1e18])
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_scores_of_large_queries_and_small_keys(dtype, outlier):
+    """Only the products have to be of ordinary size."""
+    d, n = 64, 200
+    k, v, q = randn(9, n, 1, d) / outlier, randn(10, n, 1, d), randn(11, 2, 1, d) * outlier
+    c = filled([k.to(dtype)], [v.to(dtype)])
+    q, got = c.attend([2], 1, q=q.to(dtype))
+    check(c, q, got, [0, 0])
