@@ -133,8 +133,8 @@ struct Kv8Attn {
   int n_heads, share, m_upper, len_upper;                 // share = query heads per K/V head
   int unit, pieces;                                       // slots a length is counted in; pieces wanted
   float scale_log2;                                       // scale * log2(e): probabilities are powers of two
-  // partial p: sums [16 queries][d]; behind all of them maximum and sum.  Fewer than 2 pieces: a segment of n units in k > 1
-  // pieces has k < n / c + 1 < 2 n / c, where all n together are at most c pieces
+  // partial p: results [16 queries][d], each a mean over the slots of its piece; behind all of them maximum and sum.  Fewer than
+  // 2 pieces: a segment of n units in k > 1 pieces has k < n / c + 1 < 2 n / c, where all n together are at most c pieces
   __device__ float* sums(int p, int col, int d) const { return part + ((size_t)p * 16 + col) * d; }
   __device__ float2* stats(int p, int col, int d) const { return reinterpret_cast<float2*>(part + (size_t)pieces * 32 * d) + (size_t)p * 16 + col; }
 };
@@ -442,46 +442,52 @@ __device__ __forceinline__ void Kv8Segment<T, D, ONCE>::run(const Kv8View& kv, c
     }
     if (s0 < end) ask_v();
   }
-  // the waves' partial results, 16 threads to a query (addresses from here on are worked out here: computed ahead of the loop, as
-  // the compiler would, they cost it 26 registers that it does not have)
+  // The waves' partial results, 16 threads to a query.  A wave's sums are divided by its own sum of probabilities while they are still
+  // in their power of two, and a piece's leave it divided by the piece's: a mean of finite values is finite, their sum need not be.
+  // (Addresses from here on are worked out here: computed ahead of the loop, as the compiler would, they cost it 26 registers that
+  // it does not have.)
   int tid = threadIdx.x, share = a.share;
   asm volatile("" : "+v"(tid), "+s"(share));
   l = sum_across(l);
   if constexpr (kFull) __syncthreads();                   // the sums lie where the queries were
   const int lane_e = tid & 63, col_e = lane_e & 15, grp_e = lane_e >> 4;
   if (grp_e == 0) { sh.m[wave][col_e] = m; sh.l[wave][col_e] = l; }
+  const float per = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int u = 0; u < E / 4; ++u)                     // dims (E / 4) row + u of the chunk
-        sh.o[wave][col_e][c * 4 * E + E / 4 * (4 * grp_e + e) + u] = __builtin_amdgcn_ldexpf(o[c * (E / 4) + u][e], top - kTop);
+        sh.o[wave][col_e][c * 4 * E + E / 4 * (4 * grp_e + e) + u] = __builtin_amdgcn_ldexpf(o[c * (E / 4) + u][e] * per, top - kTop);
   __syncthreads();
   constexpr int PER = D / 16;
   const int c = tid / 16, dim0 = tid % 16 * PER, fq = first + c;
   if (fq >= queries) return;
-  float best = kNegInf, sum = 0.f, acc[PER] = {};
+  float best = kNegInf, sum = 0.f, part_w[kWaves], acc[PER] = {};
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) best = fmaxf(best, sh.m[w][c]);
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     const float mw = sh.m[w][c], lw = sh.l[w][c];
-    const float part = mw == kNegInf && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - best);
-    sum = fmaf(part, lw, sum);
-#pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = fmaf(part, sh.o[w][c][dim0 + e], acc[e]);
+    part_w[w] = mw == kNegInf && lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mw - best) * lw;
+    sum += part_w[w];
   }
-  const int r = row0 + fq / a.share, h = kvh * a.share + fq % a.share;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    part_w[w] *= inv;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = fmaf(part_w[w], sh.o[w][c][dim0 + e], acc[e]);
+  }
   if (part >= 0) {
 #pragma unroll
     for (int e = 0; e < PER; ++e) a.sums(part, c, D)[dim0 + e] = acc[e];
     if (dim0 == 0) *a.stats(part, c, D) = make_float2(best, sum);
   } else {
     const int r = row0 + fq / share, h = kvh * share + fq % share;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) st<T>::stv((T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + dim0 + e, acc[e] * inv);
+    for (int e = 0; e < PER; ++e) st<T>::stv((T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + dim0 + e, acc[e]);
   }
 }
 
@@ -556,19 +562,22 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8View kv, Kv8Attn a) {
   const int f = (r - row0) * a.share + h % a.share, col = f % 16;
   const int p0 = before + (h / a.share * tiles + f / 16) * n;
   if (r < row0 || before < 0 || p0 < 0 || p0 + n > 2 * a.pieces) return;
-  float best = kNegInf, sum = 0.f;
-  for (int c = lane; c < n; c += 64) best = fmaxf(best, a.stats(p0 + c, col, D)->x);
+  // (every wave works out the same maximum and sum; of the first 64 partials a lane's own stays in registers)
+  const float2 own = lane < n ? *a.stats(p0 + lane, col, D) : make_float2(kNegInf, 0.f);
+  float best = own.x;
+  for (int c = lane + 64; c < n; c += 64) best = fmaxf(best, a.stats(p0 + c, col, D)->x);
   best = wave_max(best);
+  auto weight = [&](float2 ml) { return ml.x == kNegInf && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - best) * ml.y; };
+  float sum = weight(own);
+  for (int c = lane + 64; c < n; c += 64) sum += weight(*a.stats(p0 + c, col, D));
+  sum = wave_sum(sum);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int c0 = 0; c0 < n; c0 += 256) {
-    float w = 0.f;
-    if (c0 + (int)threadIdx.x < n) {
-      const float2 ml = *a.stats(p0 + c0 + threadIdx.x, col, D);
-      w = ml.x == kNegInf && ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - best);
-      sum = fmaf(w, ml.y, sum);
-    }
     if (c0) __syncthreads();
-    w_sh[threadIdx.x] = w;
+    float2 ml = own;
+    if ((c0 || threadIdx.x >= 64) && c0 + (int)threadIdx.x < n) ml = *a.stats(p0 + c0 + threadIdx.x, col, D);
+    w_sh[threadIdx.x] = weight(ml) * inv;                 // (past n: never read)
     __syncthreads();
     const int here = min(256, n - c0);
 #pragma unroll 4
@@ -579,18 +588,16 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8View kv, Kv8Attn a) {
     }
   }
   sum_sh[group][at] = acc;
-  __shared__ float l_sh[4];
-  sum = block_sum<256>(sum, l_sh);                        // (its barriers stand between the sums' stores and their loads)
+  __syncthreads();
   if (threadIdx.x >= D / 4) return;
 #pragma unroll
   for (int g = 1; g < kGroups; ++g) {
     const float4 p = sum_sh[g][at];
     acc.x += p.x; acc.y += p.y; acc.z += p.z; acc.w += p.w;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   T* dst = (T*)a.out + (size_t)r * a.out_stride + (size_t)h * D + at * 4;
-  const float v[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
-  if constexpr (sizeof(T) == 2) st4(dst, v); else *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+  const float v[4] = {acc.x, acc.y, acc.z, acc.w};
+  if constexpr (sizeof(T) == 2) st4(dst, v); else *reinterpret_cast<float4*>(dst) = acc;
 }
 
 struct Kv8Plan { int unit, wgs, pieces; bool once, split; };

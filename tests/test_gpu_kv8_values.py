@@ -129,3 +129,25 @@ def test_scores_of_large_queries_and_small_keys(dtype, outlier):
     c = filled([k.to(dtype)], [v.to(dtype)])
     q, got = c.attend([2], 1, q=q.to(dtype))
     check(c, q, got, [0, 0])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("d", [64, 256])
+def test_values_near_the_largest_finite_number(dtype, d):
+    """A weighted mean of finite values is finite: sums are normalised before they leave their power of two, within a wave, between
+    waves and between partial results."""
+    lens = [40, 700, 3000]
+    k, v = [0.1 * randn(12 + n, n, 1, d) for n in lens], [3e38 * (randn(13, 1, 1, d).sign() * (1 - randn(n, n, 1, 1).abs() / 64)) for n in lens]
+    c = filled([x.to(dtype) for x in k], [x.to(dtype) for x in v])
+    q, got = c.attend([1, 2, 1], 1, q=randn(14, 4, 1, d).to(dtype))
+    assert np.isfinite(got).all()
+    check(c, q, got, [0, 1, 1, 2])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_values_near_the_smallest_normal_number(dtype):
+    d, lens = 64, [40, 3000]
+    k, v = [randn(15 + n, n, 1, d) for n in lens], [2.0 ** -112 * randn(n, n, 1, d) for n in lens]
+    c = filled([x.to(dtype) for x in k], [x.to(dtype) for x in v])
+    q, got = c.attend([1, 1], 1, q=randn(16, 2, 1, d).to(dtype))
+    check(c, q, got, [0, 1])
