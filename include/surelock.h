@@ -433,9 +433,10 @@ int sl_peak_probe_stream(void *stream, const void *src, void *dst, size_t bytes,
  * multiple of 8 (the last group may be short); n, k <= 2^24, n k <= 2^34.
  *
  * sl_linear_q4_quantize: codes, scales and zeros of a plain W (dtype SL_F32 / SL_BF16), nearest code per group, all in fp32:
- * with zeros, lo = min(0, min w), hi = max(0, max w), scale = bf16((hi - lo) / 15), zero = rint(-lo / scale) in 0..15, code =
- * rint(w / scale) + zero in 0..15; without, scale = bf16(max|w| / 7), code = rint(w / scale) + 8 in 0..15.  A group of zeros has
- * scale 0; one that holds a NaN or an infinity has scale NaN, and so has every weight of it.  w is 16-byte, codes 4-byte aligned.
+ * with zeros, lo = min(0, min w), hi = max(0, max w), scale = bf16((hi - lo) / 15) (hi / 15 - lo / 15 where hi - lo overflows),
+ * zero = rint(-lo / scale) in 0..15, code = rint(w / scale) + zero in 0..15; without, scale = bf16(max|w| / 7), code =
+ * rint(w / scale) + 8 in 0..15.  A group of zeros has scale 0; one that holds a NaN or an infinity has scale NaN, and so has
+ * every weight of it.  w is 16-byte, codes 4-byte aligned.
  * sl_linear_q4_bytes / sl_linear_q4_pack: size of, and conversion into, the layout sl_linear_q4_forward reads (codes of a
  * matrix-core operand in one 16-byte load); packed is 16-byte aligned. */
 int sl_linear_q4_quantize(void *stream, const void *w, int32_t dtype, int32_t n, int32_t k, int32_t group, void *codes,

@@ -90,7 +90,8 @@ __global__ __launch_bounds__(256) void q4_quantize_kernel(const T* w, int n, int
   most = over_lanes<L>(most, larger);
   hi = over_lanes<L>(hi, larger);
   lo = over_lanes<L>(lo, [](float x, float y) { return fminf(x, y); });
-  const float raw = zeros ? (hi - lo) / 15.f : most / 7.f;
+  const float span = hi - lo;                              // infinity where all weights are finite: one at each end of fp32's range
+  const float raw = !zeros ? most / 7.f : span < __builtin_inff() ? span / 15.f : hi / 15.f - lo / 15.f;
   const bf16_t sb = (bf16_t)(most < __builtin_inff() ? raw : __builtin_nanf(""));
   const float s = (float)sb;
   const bool some = s > 0.f && s < __builtin_inff();
