@@ -444,8 +444,8 @@ int sl_linear_q4_quantize(void *stream, const void *w, int32_t dtype, int32_t n,
 int sl_linear_q4_bytes(int32_t n, int32_t k, int32_t group, size_t *out);
 int sl_linear_q4_pack(void *stream, const void *codes, const void *scales, const void *zeros, int32_t n, int32_t k,
                       int32_t group, void *packed, size_t packed_bytes);
-/* y = x W^T for the first min(*m_dev, m_upper) rows of x [m_upper, k] (bf16, row-major, 16-byte aligned), accumulated in fp32;
- * exactly one of
+/* y = x W^T for the first min(*m_dev, m_upper) rows of x [m_upper, k] (bf16, row-major, 16-byte aligned), accumulated in fp32.
+ * packed is what sl_linear_q4_pack wrote for the same n, k and group: sl_linear_q4_bytes bytes of it are read.  Exactly one of
  *   y_f32  [m_upper, n] fp32, or
  *   y_bf16 [*, n] bf16, row r written to row row_map[r] (row_map may be null; only with y_bf16)
  * is non-null.  Rows past the count are neither read nor written.  A row that holds a NaN or an infinity, or whose sums leave

@@ -2,6 +2,7 @@
 torch tensors (device memory) and Python ints.  Argument marshalling only: every step of the
 path runs in the HIP kernels.  There is no fallback: a missing library raises."""
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -359,13 +360,21 @@ def _here():
     return dev, torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _addr(t, dtype, dev):
-    """Address of a dense tensor (or None)."""
+def _addr(t, dtype, dev, least=0):
+    """Address of a dense tensor (or None) of at least `least` elements: what the call reads or writes of it."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"a contiguous {dtype} tensor on cuda:{dev} is needed, not {t.dtype}, strides {t.stride()}, on {t.device}")
+    if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"a contiguous {dtype} tensor of at least {least} elements on cuda:{dev} is needed, not {tuple(t.shape)} {t.dtype}, "
+                         f"strides {t.stride()}, on {t.device}")
     return t.data_ptr()
+
+
+def _float_code(t):
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"float32 or bfloat16 is needed, not {t.dtype}")
+    return code
 
 
 def _require_gpu(t):
@@ -377,13 +386,24 @@ _F32, _BF16, _I32, _U8 = torch.float32, torch.bfloat16, torch.int32, torch.uint8
 
 
 # ---- 4-bit weights ---------------------------------------------------------------------------
+@functools.lru_cache(maxsize=1024)
+def _q4_sizes(n, k, group):
+    """Elements of (a row of x, a row of y, the codes, the scales, the packed weights); zeros for a shape that the library refuses, which
+    is then left to the call to report."""
+    out = _Z()
+    if lib().sl_linear_q4_bytes(n, k, group, C.byref(out)):
+        return 0, 0, 0, 0, 0
+    return k, n, n * (k // 2), n * -(-k // group), out.value
+
+
 def sl_linear_q4_quantize(w, group, codes, scales, zeros=None):
     """w [n, k]; codes [n, k/2] uint8, scales [n, ceil(k/group)] bfloat16, zeros likewise uint8 or None (see the header)."""
     _require_gpu(w)
     dev, stream = _here()
     n, k = w.shape
-    _check("sl_linear_q4_quantize", lib().sl_linear_q4_quantize(stream, _addr(w, w.dtype, dev), dtype_code(w.dtype), n, k, group,
-                                                                _addr(codes, _U8, dev), _addr(scales, _BF16, dev), _addr(zeros, _U8, dev)))
+    _, _, n_codes, n_scales, _ = _q4_sizes(n, k, group)
+    _check("sl_linear_q4_quantize", lib().sl_linear_q4_quantize(stream, _addr(w, w.dtype, dev), _float_code(w), n, k, group, _addr(codes, _U8, dev, n_codes),
+                                                                _addr(scales, _BF16, dev, n_scales), _addr(zeros, _U8, dev, n_scales)))
 
 
 def sl_linear_q4_bytes(n, k, group):
@@ -395,17 +415,22 @@ def sl_linear_q4_bytes(n, k, group):
 def sl_linear_q4_pack(codes, scales, zeros, n, k, group, packed):
     _require_gpu(codes)
     dev, stream = _here()
-    _check("sl_linear_q4_pack", lib().sl_linear_q4_pack(stream, _addr(codes, _U8, dev), _addr(scales, _BF16, dev), _addr(zeros, _U8, dev), n, k,
-                                                        group, _addr(packed, _U8, dev), packed.numel()))
+    _, _, n_codes, n_scales, _ = _q4_sizes(n, k, group)
+    _check("sl_linear_q4_pack", lib().sl_linear_q4_pack(stream, _addr(codes, _U8, dev, n_codes), _addr(scales, _BF16, dev, n_scales),
+                                                        _addr(zeros, _U8, dev, n_scales), n, k, group, _addr(packed, _U8, dev), packed.numel()))
 
 
 def sl_linear_q4_forward(x, packed, m_dev, m_upper, n, k, group, y_f32=None, y_bf16=None, row_map=None):
+    """x [m_upper, k], y_f32 or y_bf16 [m_upper, n] ([*, n] with row_map [m_upper], whose rows the caller answers for)."""
     _require_gpu(x)
     if m_upper == 0:                       # (empty tensors have no address)
         return
     dev, stream = _here()
-    status = lib().sl_linear_q4_forward(stream, _addr(x, _BF16, dev), _addr(packed, _U8, dev), _addr(m_dev, _I32, dev), m_upper, n, k, group,
-                                        _addr(y_f32, _F32, dev), _addr(y_bf16, _BF16, dev), _addr(row_map, _I32, dev))
+    x_row, y_row, _, _, n_packed = _q4_sizes(n, k, group)
+    y_least = m_upper * y_row
+    status = lib().sl_linear_q4_forward(stream, _addr(x, _BF16, dev, m_upper * x_row), _addr(packed, _U8, dev, n_packed), _addr(m_dev, _I32, dev, 1),
+                                        m_upper, n, k, group, _addr(y_f32, _F32, dev, y_least),
+                                        _addr(y_bf16, _BF16, dev, y_least if row_map is None else y_row), _addr(row_map, _I32, dev, m_upper))
     if status:
         raise SureLockError("sl_linear_q4_forward", status)
 
@@ -421,14 +446,19 @@ class KV8:
         self.device = page_table.get_device()
         if pool is not None and pool.device != page_table.device:
             raise ValueError(f"the pool is on {pool.device}, its page table on {page_table.device}")
+        if pool is not None and (not pool.is_contiguous() or _nbytes(pool) < need):
+            raise ValueError(f"a contiguous pool of at least {need} bytes is needed, not {_nbytes(pool)}, strides {pool.stride()}")
         self.pool = torch.empty(need, dtype=torch.uint8, device=page_table.device) if pool is None else pool
         self.page_table, self.n_kv_heads, self.d_head = page_table, n_kv_heads, d_head
-        batch, max_pages = page_table.shape
+        self.batch, max_pages = page_table.shape
         self.desc = sl_kv8(_ptr(self.pool), _nbytes(self.pool), _addr(page_table, _I32, self.device), n_pages, page_slots,
-                           n_kv_heads, d_head, batch, max_pages)
+                           n_kv_heads, d_head, self.batch, max_pages)
         self.desc_ref = C.byref(self.desc)
 
     def sequence(self, b):
+        if not -self.batch <= b < self.batch:
+            raise IndexError(f"sequence {b} of {self.batch}")
+        b %= self.batch
         return KV8(self.desc.n_pages, self.desc.page_slots, self.n_kv_heads, self.d_head, self.page_table[b:b + 1], self.pool)
 
 
@@ -446,12 +476,13 @@ def _kv8_here(kv):
     return dev, stream
 
 
-def _head_rows(t, dtype, dev, heads, d):
-    """(address, row stride in elements) of rows [*, heads, d] that may lie apart; a row itself is dense."""
+def _head_rows(t, dtype, dev, heads, d, least):
+    """(address, row stride in elements) of at least `least` rows [*, heads, d] that may lie apart; a row itself is dense."""
     shape, st = t.shape, t.stride()
-    if t.dtype is not dtype or t.get_device() != dev or len(shape) != 3 or shape[1] != heads or shape[2] != d or st[2] != 1 or (
+    if t.dtype is not dtype or t.get_device() != dev or len(shape) != 3 or shape[0] < least or shape[1] != heads or shape[2] != d or st[2] != 1 or (
             st[1] != d and heads > 1):
-        raise ValueError(f"rows of [{heads}, {d}] {dtype} on cuda:{dev} are needed, not {tuple(shape)} {t.dtype}, strides {st}, on {t.device}")
+        raise ValueError(f"at least {least} rows of [{heads}, {d}] {dtype} on cuda:{dev} are needed, not {tuple(shape)} {t.dtype}, strides {st}, "
+                         f"on {t.device}")
     return t.data_ptr(), st[0] if shape[0] > 1 else heads * d
 
 
@@ -461,8 +492,8 @@ def _kv8_rows(name, fn, kv, k, v, row_pos, cu_rows, m_upper):
         return
     dev, stream = _kv8_here(kv)
     dtype, heads, d = k.dtype, kv.n_kv_heads, kv.d_head
-    (kp, ks), (vp, vs) = _head_rows(k, dtype, dev, heads, d), _head_rows(v, dtype, dev, heads, d)
-    status = fn(stream, kv.desc_ref, kp, vp, _DTYPE_CODES[dtype], ks, vs, _addr(row_pos, _I32, dev), _addr(cu_rows, _I32, dev), m_upper)
+    (kp, ks), (vp, vs) = _head_rows(k, dtype, dev, heads, d, m_upper), _head_rows(v, dtype, dev, heads, d, m_upper)
+    status = fn(stream, kv.desc_ref, kp, vp, _float_code(k), ks, vs, _addr(row_pos, _I32, dev, m_upper), _addr(cu_rows, _I32, dev, kv.batch + 1), m_upper)
     if status:
         raise SureLockError(name, status)
 
@@ -488,9 +519,9 @@ def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, wo
         return
     dev, stream = _kv8_here(kv)
     dtype, n_heads, d = q.dtype, q.shape[1], kv.d_head
-    (qp, qs), (op, os_) = _head_rows(q, dtype, dev, n_heads, d), _head_rows(out, dtype, dev, n_heads, d)
-    status = lib().sl_kv8_attention(stream, kv.desc_ref, qp, _DTYPE_CODES[dtype], qs, n_heads, _addr(cu_rows, _I32, dev),
-                                    _addr(seq_len, _I32, dev), _addr(row_len, _I32, dev), m_upper, len_upper, scale, op, os_,
+    (qp, qs), (op, os_) = _head_rows(q, dtype, dev, n_heads, d, m_upper), _head_rows(out, dtype, dev, n_heads, d, m_upper)
+    status = lib().sl_kv8_attention(stream, kv.desc_ref, qp, _float_code(q), qs, n_heads, _addr(cu_rows, _I32, dev, kv.batch + 1),
+                                    _addr(seq_len, _I32, dev, kv.batch), _addr(row_len, _I32, dev, m_upper), m_upper, len_upper, scale, op, os_,
                                     _addr(workspace, _U8, dev), workspace.numel())
     if status:
         raise SureLockError("sl_kv8_attention", status)
