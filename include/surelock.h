@@ -488,7 +488,7 @@ int sl_kv8_read(void *stream, const sl_kv8 *kv /* host */, void *k, void *v, int
 /* Attention of each row over the slots of its sequence:
  *   out[r, h] = sum_p softmax_p(scale * q[r, h] . K[p, h / share]) V[p, h / share],  share = n_heads / n_kv_heads,
  * p over the first min(seq_len[b], row_len[r]) slots (no more than the table's and than len_upper), without those on no page.
- * A row that sees no slot gets zeros.  n_heads <= 2^14, m_upper <= 2^20, their product <= 2^27; scale positive and finite.
+ * A row that sees no slot gets zeros.  n_heads <= 2^14, m_upper <= 2^20, their product <= 2^27; scale positive, scale log2(e) finite.
  *   q, out   [m_upper] rows of [n_heads, d_head] (dtype), q_stride / out_stride elements apart, aligned as above; out must not
  *            overlap q
  *   seq_len  [batch] i32;  row_len [m_upper] i32, or null: every row sees its whole sequence

@@ -820,7 +820,7 @@ extern "C" int sl_kv8_attention(void* stream, const sl_kv8* kv, const void* q, i
   if (!cu_rows || !seq_len || !workspace || (uintptr_t)workspace % 256 || (dtype != SL_F32 && dtype != SL_BF16)) return SL_EINVAL;
   const int64_t width = (int64_t)n_heads * kv->d_head;
   if (!kv8_rows_ok(q, q_stride, width, dtype) || !kv8_rows_ok(out, out_stride, width, dtype)) return SL_EINVAL;
-  if (!(scale > 0.f) || !(scale < __builtin_inff())) return SL_EINVAL;
+  if (!(scale > 0.f) || !((float)(scale * 1.4426950408889634) < __builtin_inff())) return SL_EINVAL;      // (scores are in powers of two)
   if (m_upper == 0) return SL_OK;
   const Kv8View v = kv8_view(kv);
   if (workspace_bytes < slk_kv8_attention_bytes(v, kv->d_head, n_heads, m_upper, len_upper)) return SL_ENOSPC;

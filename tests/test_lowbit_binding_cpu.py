@@ -147,3 +147,12 @@ def test_one_sequence_of_a_cache(library):
     for b in (2, -3):
         with pytest.raises(IndexError):
             kv.sequence(b)
+
+
+# ---- the library's own refusal ----------------------------------------------------------------------
+def test_a_scale_that_overflows_in_powers_of_two_is_refused():
+    """Scores are taken in powers of two, so scale log2(e) has to be finite (2.35e38 is, 2.37e38 is not)."""
+    kv = B.C.byref(B.sl_kv8(256, 1 << 40, 256, 10, 64, 4, 128, 2, 5))
+    call = lambda scale: B.lib().sl_kv8_attention(None, kv, 256, 1, 1024, 8, 256, 256, None, 0, 100, scale, 256, 1024, 256, 1 << 40)  # noqa: E731
+    assert call(2.35e38) == B.SL_OK                           # (no rows: nothing to launch)
+    assert call(2.37e38) == B.SL_EINVAL and call(3.4e38) == B.SL_EINVAL
