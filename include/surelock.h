@@ -449,9 +449,12 @@ int sl_linear_q4_pack(void *stream, const void *codes, const void *scales, const
  *   y_f32  [m_upper, n] fp32, or
  *   y_bf16 [*, n] bf16, row r written to row row_map[r] (row_map may be null; only with y_bf16)
  * is non-null.  Rows past the count are neither read nor written.  A row that holds a NaN or an infinity, or whose sums leave
- * fp32's range when multiplied by 15, comes out as NaN (sums over codes and over zero points are taken apart).  No workspace;
- * the same sums in the same order in every call of one m_upper.  m_upper <= 2^20.  Made for few rows: weights are unpacked
- * again for every 32 rows, so hundreds of rows are a matter of that, and thousands better served by sl_linear_forward. */
+ * fp32's range when multiplied by 15, comes out as NaN (sums over codes and over zero points are taken apart); a column with a
+ * scale that is not finite comes out as NaN or an infinity.  No workspace; the same sums in the same order in every call of one
+ * m_upper, n, k and group.  m_upper <= 2^20.
+ * Made for few rows: weights are unpacked again for every 32 rows.  Against sl_linear_forward with bf16 weights (both from
+ * memory): 12288 x 4096, 16 rows 9 us for 47, 128 rows 27 for 56, 384 rows 63 for 69, 512 rows 77 for 67.  The products inside a
+ * layer (sl_forward_layers) are faster than sl_linear_forward at few rows, and level with this call near 64. */
 int sl_linear_q4_forward(void *stream, const void *x, const void *packed, const int32_t *m_dev, int32_t m_upper,
                          int32_t n, int32_t k, int32_t group, float *y_f32, void *y_bf16, const int32_t *row_map);
 
@@ -476,7 +479,8 @@ int sl_kv8_bytes(int32_t n_pages, int32_t page_slots, int32_t n_kv_heads, int32_
  *   k, v     [m_upper] rows of [n_kv_heads, d_head] (dtype SL_F32 / SL_BF16), k_stride / v_stride elements apart (a
  *            projection's fused output has such strides); 16-byte aligned, strides a multiple of 16 bytes
  *   cu_rows  [batch + 1] i32: rows cu_rows[b] .. cu_rows[b + 1] - 1 belong to sequence b (cu_active of a step is one such)
- *   row_pos  [m_upper] i32: the row's slot in its sequence;  m_upper <= 2^20
+ *   row_pos  [m_upper] i32: the row's slot in its sequence (a step's active_idx counts over all sequences: slot = id - b N);
+ *            m_upper <= 2^20
  * Rows from cu_rows[batch] on are left alone.  A row whose slot is negative, past the table or on no page is not written;
  * read back it is zeros.  Of adjacent rows that name one slot the last is kept; rows that name one slot must be
  * adjacent.  Values read back are code * scale in fp32, rounded to dtype.  A page may be shared by sequences that read it;
@@ -496,9 +500,11 @@ int sl_kv8_read(void *stream, const sl_kv8 *kv /* host */, void *k, void *v, int
  *   workspace      sl_kv8_attention_bytes bytes, 256-byte aligned; needs no initialisation, two calls that may overlap in time
  *                  must not share one
  * Rows from cu_rows[batch] on are left as they are.  Scores, softmax statistics and sums are fp32.  fp32 queries and weights
- * (probability times V's scale) keep 24 bits each; of bf16 queries, numbers below 2^-15 of their head's largest lose the bits
- * under 2^-23 of it, and bf16 weights have 22 bits or, if coarser, 2^-39 of the row's largest.  The same sums in the same order in
- * every call of the same bounds (no atomics). */
+ * (probability times V's scale) keep 24 bits each.  Of bf16 queries, numbers below 2^-15 of their head's largest lose the bits
+ * under 2^-23 of it; bf16 weights have 22 bits or, if coarser, 2^-39 of the row's largest; and a bf16 row whose sum of |q| times
+ * 184 scale leaves fp32's range may come out as NaN.  A weighted mean of finite values is finite.  No atomics: calls that agree
+ * in bounds and in all sequences' row counts and lengths add up in the same order and agree in every bit.  (A sequence is cut by
+ * what the others leave of the chip, so its last bits may change when another one grows.) */
 int sl_kv8_attention_bytes(const sl_kv8 *kv /* host */, int32_t n_heads, int32_t m_upper, int32_t len_upper, size_t *out);
 int sl_kv8_attention(void *stream, const sl_kv8 *kv /* host */, const void *q, int32_t dtype, int64_t q_stride, int32_t n_heads,
                      const int32_t *cu_rows, const int32_t *seq_len, const int32_t *row_len, int32_t m_upper,

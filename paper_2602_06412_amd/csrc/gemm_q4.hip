@@ -66,7 +66,8 @@ __device__ inline float over_lanes(float v, F f) {
 }
 
 // Range, scale, zero point and codes; eight numbers a lane, group / 8 lanes a group.  24576 x 4096 bf16 take 92 us (253 MB, 2.8 TB/s:
-// the quotients' divisions are taken to bound it; it runs once, when weights are loaded); a thread for each group took 3.7 ms.
+// bound by vector instructions, 310 a wave, the pipes busy throughout; it runs once, when weights are loaded); a thread for each group
+// took 3.7 ms.
 template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void q4_quantize_kernel(const T* w, int n, int k, int groups, unsigned char* codes, bf16_t* scales, unsigned char* zeros) {
   constexpr int L = GROUP / 8;
@@ -135,7 +136,8 @@ __device__ inline float sum_of_piece(const uint4& v) {
 //
 // Rows pass through LDS, once for the WN waves of a group, and with them goes the sum of each group of weights' inputs.  An
 // operand has 16 rows side by side in a wave's lanes, and loaded so from row-major memory every lane is an access of its own (16
-// bytes a cycle of the address unit, which was busy 70 % of the time: 61 rows, n = 4096, k = 12288 took 53 us for 33).  Here eight
+// bytes a cycle of the address unit, which was busy 70 % of the time: 61 rows, n = 4096, k = 12288 took 53 us; 33 through LDS with the
+// rest as it was, 18 to 21 now).  Here eight
 // lanes take a row's 128 consecutive bytes; 16-byte pieces that would meet in one bank are kept apart by an exclusive or of their row
 // with their place.
 template <int GS, int MT, int CT, int WN, int WK, int U>
@@ -309,19 +311,32 @@ int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int g
 
 int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
                   void* y_bf16, const int32_t* row_map) {
-  // Tiles, us by tile (rows x columns, waves side by side x along the reduction):
+  // Tiles, us by tile (rows x columns, waves side by side x along the reduction), a node of a graph over four sets of weights, groups of
+  // 128; * is what the rule takes:
   //   n, k, rows            16x16,1x16  16x32,1x8  16x48,1x8  32x32,1x8  32x128,4x2
-  //   4096, 4096, 1             6.5        7.7        8.4        9.5        18
-  //   4096, 12288, 16          11.7       15.7       19.2       21.7        58
-  //   12288, 4096, 16          13.5       10.7        9.9       14.0        19
-  //   24576, 4096, 8           21.6       13.5       13.3       18.5        19
-  //   4096, 4096, 32            9.5        7.7        9.0        9.9        18
-  //   4096, 12288, 61          37.6       26.7       31.1       23.9        58
-  //   12288, 4096, 100         65         36         34         33          28
-  //   24576, 4096, 224        256        136        126        114          81
+  //   4096, 4096, 1             4.8 *      6.0        6.8        7.7        16.4
+  //   4096, 12288, 16           9.4 *     13.0       15.2       17.4        43.6
+  //   4096, 2048, 1             3.5 *      3.8        4.4        4.8         8.7
+  //   4096, 1920, 1             3.5        3.9 *      4.5        5.1         9.3
+  //   4096, 1024, 1             3.5        3.1 *      3.4        3.7         5.6
+  //   4352, 4096, 1             7.3        6.1 *      6.9        7.8        16.4
+  //   8192, 4096, 16            8.0        6.4 *      7.3        8.1        16.6
+  //   8704, 4096, 16           10.7        8.4        7.3 *     11.1        16.7
+  //   12288, 4096, 16          11.2        8.8        7.8 *     11.7        16.8
+  //   24576, 4096, 8           19.5       11.8       11.7 *     16.3        17.6
+  //   4096, 4096, 32            7.8        6.2 *      7.3        8.3        17.1
+  //   4096, 12288, 61          30.2       20.2       26.1       18.3 *      44.0
+  //   12288, 4096, 48          28.7       16.7       15.0       17.1        17.3 *
+  //   4096, 4096, 128          24.6       13.8       15.6       12.2 *      17.0
+  //   6144, 4096, 100          32.7       18.2       17.5       16.7        17.0 *
+  //   12288, 4096, 64          37.5       19.7       18.7       18.0        17.4 *
+  //   12288, 4096, 100         62.9       32.4       29.5       30.6        24.6 *
+  //   24576, 4096, 224        254        131        122        110          75.3 *
   // Few rows are a matter of the weights' latency: workgroups enough for all CUs, many waves along the reduction, and as many columns as
-  // still leave one workgroup to a CU.  Many rows are a matter of unpacking weights and of moving rows: a large tile whose waves share
-  // them, once there are enough of it.
+  // still leave one workgroup to a CU.  16 waves want 16 blocks to share out: with 15 the rule is 10 % off, with 8 eight waves are the
+  // better ones.  Many rows are a matter of unpacking weights and of moving rows: a large tile whose waves share them, once there are
+  // enough of it; at 192 workgroups of it the two are within 4 %, at 128 it takes 1.4 times as long, at 384 0.8.  (33 to 48 rows of wide
+  // matrices are 15 % off: three row tiles in the room of four.)
   const int64_t rows16 = sl_cdiv(m_upper, 16), tiles_n = sl_cdiv(n, kCols), blocks_k = sl_cdiv(k, kDepth);
 #define Q4_RUN(GS, MT, CT, WN, WK, U)                                                                                                  \
   hipLaunchKernelGGL((q4_linear_kernel<GS, MT, CT, WN, WK, U>), dim3(sl_cdiv(n, kCols * CT * WN), sl_cdiv(m_upper, 16 * MT)),          \

@@ -53,7 +53,8 @@ template <> struct Piece<16> {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
 };
-// (loads of codes that no other workgroup asks for go past the caches' replacement: the loads alone, of 830 MB, 133 us instead of 153)
+// (loads of codes that no other workgroup asks for go past the caches' replacement: the loads alone, 830 MB of twelve sequences of like
+// length, 133 us instead of 153)
 template <bool ONCE, typename P>
 __device__ inline P ask(const P* p) {
   return ONCE ? __builtin_nontemporal_load(p) : *p;
@@ -113,11 +114,13 @@ __device__ inline void signed_bytes(const float (&x)[4], uint32_t (&w)[3]) {
 }
 
 constexpr int kResident = 3;                              // workgroups of a CU that registers let run at once (2 with d = 256)
-// Pieces wanted, in rounds of what runs at once.  us at 1, 2, 3, 4, 6 rounds: one row in each of 8 ragged sequences 59, 52, 55, 56, 61;
-// 16 long ragged ones 162, 156, 149, 153, 160; one longer round ends when its last workgroup does, many short ones start often.
+// Pieces wanted, in rounds of what runs at once.  us at 1, 2, 3, 4 rounds (heads of 128 but where stated): one row in each of 8 ragged
+// sequences 60, 53, 57, 57; 16 long ragged ones 163, 157, 151, 155; 12 long ones of like length 135, 136, 141, 141; 16 rows of 64
+// heads over 8 97, 78, 79, 101; 64 rows of 2048 slots 22.7, 22.7, 23.5, 23.9; ragged ones of 256 a head 37, 43, 43, 43.  One longer
+// round ends when its last workgroup does, many short ones start often; two are never far from the best.
 constexpr int kRounds = 2;
-// Units of a piece, at least (us at 1, 2, 4: 64 rows of 2048 slots 25.7, 25.9, 22.5; one row of 4096 slots 18.5, 16.6, 17.4): up to
-// 512 slots a segment is one piece and the second launch falls away.
+// Units of a piece, at least; up to 512 slots a segment is one piece and the second launch falls away.  us at 1, 2, 4, 8: 64 rows of
+// 2048 slots 25.9, 26.0, 22.7, 25.1; one row of 4096 slots 18.5, 16.8, 17.7, 23.3; one row in each of 8 ragged sequences 53, 53, 53, 58.
 constexpr int kLeast = 4;
 
 // A segment is a tile of queries with one K/V head: sequence by sequence, head by head, tile by tile.  Segments are cut into pieces of

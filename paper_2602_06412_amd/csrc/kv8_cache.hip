@@ -10,8 +10,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // slot of K.  A quad's wave belongs to the first of the adjacent rows that share it; rows of a prompt so come four at a time,
 // scattered rows one by one, and of rows that name the same slot one wave sees all and keeps the last.
 //
-// Bound by memory where rows are many: 5533 rows of 32 heads x 128 in bf16, 91 MB read and 47 written, take 42 us (a copy of as many
-// bytes 29), read back 26 us.  A wave for each row and head with byte stores took 103 and 76; all loads of a quad before its first
+// Where rows are many, 5533 rows of 32 heads x 128 in bf16, 91 MB read and 47 written, take 42 us (a copy of as many bytes 29): vector
+// instructions beside memory, 890 a wave, the pipes busy 68 % of the time.  Read back 26 us, which is memory.  A wave for each row and head with byte stores took 103 and 76; all loads of a quad before its first
 // conversion, and the positions of its rows in one load by the lanes, were 73 to 42.
 template <int D>
 struct Quad {
