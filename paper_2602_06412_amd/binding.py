@@ -427,10 +427,12 @@ def sl_linear_q4_forward(x, packed, m_dev, m_upper, n, k, group, y_f32=None, y_b
         return
     dev, stream = _here()
     x_row, y_row, _, _, n_packed = _q4_sizes(n, k, group)
-    y_least = m_upper * y_row
+    if row_map is None:
+        y_row *= m_upper
     status = lib().sl_linear_q4_forward(stream, _addr(x, _BF16, dev, m_upper * x_row), _addr(packed, _U8, dev, n_packed), _addr(m_dev, _I32, dev, 1),
-                                        m_upper, n, k, group, _addr(y_f32, _F32, dev, y_least),
-                                        _addr(y_bf16, _BF16, dev, y_least if row_map is None else y_row), _addr(row_map, _I32, dev, m_upper))
+                                        m_upper, n, k, group, None if y_f32 is None else _addr(y_f32, _F32, dev, y_row),
+                                        None if y_bf16 is None else _addr(y_bf16, _BF16, dev, y_row),
+                                        None if row_map is None else _addr(row_map, _I32, dev, m_upper))
     if status:
         raise SureLockError("sl_linear_q4_forward", status)
 
@@ -521,7 +523,8 @@ def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, wo
     dtype, n_heads, d = q.dtype, q.shape[1], kv.d_head
     (qp, qs), (op, os_) = _head_rows(q, dtype, dev, n_heads, d, m_upper), _head_rows(out, dtype, dev, n_heads, d, m_upper)
     status = lib().sl_kv8_attention(stream, kv.desc_ref, qp, _float_code(q), qs, n_heads, _addr(cu_rows, _I32, dev, kv.batch + 1),
-                                    _addr(seq_len, _I32, dev, kv.batch), _addr(row_len, _I32, dev, m_upper), m_upper, len_upper, scale, op, os_,
+                                    _addr(seq_len, _I32, dev, kv.batch), None if row_len is None else _addr(row_len, _I32, dev, m_upper),
+                                    m_upper, len_upper, scale, op, os_,
                                     _addr(workspace, _U8, dev), workspace.numel())
     if status:
         raise SureLockError("sl_kv8_attention", status)
