@@ -151,3 +151,24 @@ def test_values_near_the_smallest_normal_number(dtype):
     c = filled([x.to(dtype) for x in k], [x.to(dtype) for x in v])
     q, got = c.attend([1, 1], 1, q=randn(16, 2, 1, d).to(dtype))
     check(c, q, got, [0, 1])
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_numbers_that_are_not_finite_stay_with_their_rows(dtype):
+    """A NaN or an infinity in a query or in a slot that it sees makes that query's result NaN; every other one is exact, and a row that
+    sees nothing is zeros whatever its query holds."""
+    d, n = 64, 700
+    k, v = randn(20, n, 2, d), randn(21, n, 2, d)
+    c = filled([k.to(dtype)], [v.to(dtype)])
+    broken_k, broken_v = k.clone(), v.clone()
+    broken_k[600, 0, 3], broken_v[650, :, 5] = float("nan"), -float("inf")
+    B.sl_kv8_write(c.kv, broken_k.to(dtype).to(DEV), broken_v.to(dtype).to(DEV), i32(range(n)), i32([0, n]), n)
+    limits = [500, 600, 601, 651, 0, 300, 1]
+    q = randn(22, 7, 2, d)
+    q[4], q[5, 1, 7] = float("nan"), float("inf")
+    q, got = c.attend([7], 1, row_len=limits, q=q.to(dtype))
+    assert (got[4] == 0).all()
+    assert np.isnan(got[2, 0]).all() and np.isnan(got[3]).all() and np.isnan(got[5, 1]).all()
+    for r, h in ((0, 0), (0, 1), (1, 0), (1, 1), (2, 1), (5, 0), (6, 0), (6, 1)):
+        want, bound = attention(ref.f64(q[r, h]), c.K[0][:limits[r], h], c.V[0][:limits[r], h], 1.0 / math.sqrt(d), dtype)
+        assert (np.abs(got[r, h] - want) <= bound).all(), (r, h)
