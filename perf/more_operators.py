@@ -47,13 +47,13 @@ def listed():
          "rows": 262144, "max_pages": 1024},
         # three rows of the tiny model: launch and latency
         {"name": "rope_tiny_m3", "kind": "rope", "rows": 3, "heads": TINY_HEADS, "kv_heads": TINY_HEADS, "d": TINY_HEAD, "rot": TINY_HEAD, "interleaved": False,
-         "in": "fp32", "out": "fp32", "most": 128, "scaling": "none"},
+         "in": "fp32", "out": "fp32", "most": 128, "scaling": "plain"},
         # a late step of a batch of eight with long sequences: fp32 from a product, bf16 for the cache, half of the head turned, neighbours in pairs
         {"name": "rope_m137_long", "kind": "rope", "rows": 137, "heads": LLADA_HEADS, "kv_heads": 8, "d": LLADA_HEAD, "rot": 64, "interleaved": True,
          "in": "fp32", "out": "bf16", "most": 1000000, "scaling": "turns"},
         # the first step of a batch of eight ragged sequences, as columns of the fused projection
         {"name": "rope_8_prompts", "kind": "rope", "rows": 5533, "heads": LLADA_HEADS, "kv_heads": LLADA_HEADS, "d": LLADA_HEAD, "rot": LLADA_HEAD,
-         "interleaved": False, "in": "bf16", "out": "bf16", "most": 1024, "scaling": "none"},
+         "interleaved": False, "in": "bf16", "out": "bf16", "most": 1024, "scaling": "plain"},
         # one row of one request beside the Out projection: launch and latency
         {"name": "adapters_out_m1", "kind": "adapters", "rows": 1, "n": LLADA_D, "k": LLADA_D, "slots": 4, "max_rank": 16, "run": 1, "splits": 1, "out": "fp32"},
         # 64 requests of one row, an adapter each, beside the fused Q|K|V projection
@@ -129,7 +129,7 @@ def draw(rng):
             kv = rng.choice([1, 2, 4, 8, 32])
             c = {"kind": kind, "rows": _log_int(rng, 1, 8192), "heads": kv * (rng.choice([1, 2, 4, 8]) if kv < 32 else 1), "kv_heads": kv, "d": d,
                  "rot": rng.choice([d, d, d // 2, d // 4]), "interleaved": rng.random() < 0.5, "in": rng.choice(["bf16", "fp32"]),
-                 "out": rng.choice(["bf16", "bf16", "fp32"]), "most": _log_int(rng, 100, 1000000), "scaling": rng.choice(["none", "linear", "base", "turns"])}
+                 "out": rng.choice(["bf16", "bf16", "fp32"]), "most": _log_int(rng, 100, 1000000), "scaling": rng.choice(["plain", "linear", "base", "turns"])}
         elif kind == "adapters":
             c = {"kind": kind, "rows": _log_int(rng, 1, 2048), "n": rng.choice([_log_int(rng, 64, 2 * LLADA_FF), 8 * _log_int(rng, 8, LLADA_FF // 4), LLADA_D]),
                  "k": rng.choice([8 * _log_int(rng, 8, LLADA_FF // 8), TINY_D, TINY_FF, LLADA_D, LLADA_FF]), "slots": _log_int(rng, 1, 64),
@@ -213,7 +213,7 @@ def _rope_inputs(c, seed):
 
 
 ROPE = {"theta": 10000.0, "factor": 8.0, "original_len": 8192.0, "low_turns": 1.0, "high_turns": 4.0}
-AMPLITUDE = {"none": 1.0, "linear": 1.0, "base": 1.0, "turns": 1.2079}
+AMPLITUDE = {"plain": 1.0, "linear": 1.0, "base": 1.0, "turns": 1.2079}
 
 
 def _adapter_of_rows(c, seed):
@@ -283,7 +283,7 @@ def prepare(case, seed):
         st["m"] = _ints([c["rows"]])
         if own:
             st["freqs"] = torch.empty(c["rot"] // 2, dtype=torch.float64, device=DEV)
-            B.sl_rope_freqs(st["freqs"], ROPE["theta"], **({} if c["scaling"] == "none" else dict(ROPE, theta=ROPE["theta"], scaling=c["scaling"])))
+            B.sl_rope_freqs(st["freqs"], ROPE["theta"], **({} if c["scaling"] == "plain" else dict(ROPE, theta=ROPE["theta"], scaling=c["scaling"])))
             st["q_out"], st["k_out"] = (torch.empty(t.shape, dtype=_dtype(c["out"]), device=DEV) for t in (st["q"], st["k"]))
         else:
             st["freqs"] = _freqs(c)
