@@ -510,6 +510,127 @@ int sl_kv8_attention(void *stream, const sl_kv8 *kv /* host */, const void *q, i
                      const int32_t *cu_rows, const int32_t *seq_len, const int32_t *row_len, int32_t m_upper,
                      int32_t len_upper, float scale, void *out, int64_t out_stride, void *workspace, size_t workspace_bytes);
 
+/* ---- one serving step of many requests --------------------------------------------------------
+ * What stands around the low-bit calls when requests of different lengths are served together: room in the paged cache, rotary
+ * positions, each request's own low-rank weights beside a shared projection, and the draw of tokens.  They take no context. */
+
+/* Pages of a cache, handed out on the device.  One such state serves the caches of all layers (they share the page table).
+ * The struct is a HOST struct of device pointers (4-byte aligned), read during the call. */
+typedef struct sl_kv8_pages {
+  int32_t *page_table;           /* [batch][max_pages]: as sl_kv8.page_table; -1 where a sequence holds no page      */
+  int32_t *seq_len;              /* [batch] slots of each sequence; it holds ceil(seq_len / page_slots) pages        */
+  int32_t *free_pages;           /* [n_pages]: a stack, of which the first n_free[0] entries count                   */
+  int32_t *n_free;               /* [1]                                                                              */
+  int32_t n_pages, page_slots;   /* 1 .. 2^30 pages; page_slots as in sl_kv8                                         */
+  int32_t batch, max_pages;      /* as in sl_kv8; batch * max_pages <= 2^30                                          */
+} sl_kv8_pages;
+/* Empty sequences, every page free; pages come off the stack in ascending order. */
+int sl_kv8_pages_init(void *stream, const sl_kv8_pages *pages /* host */);
+/* Bring every sequence to want_len[b] slots (negative: as it is), and list the new slots as rows for sl_kv8_write.
+ *   First every sequence that wants less gives up its last pages (0: all of them).  Then, in order of b, each that wants more gets
+ *   its pages if enough pages are left, and rows of m_upper for all its new slots; if not, or beyond max_pages pages, it stays as it
+ *   is (seq_len says so) and those behind it get what they still can.  Pages given up are taken first, in the order in which they were
+ *   given up (b, then place), the rest from the top of the stack; what is given up and not taken goes on top of the stack.
+ *   from, to    the state before and after: the same struct contents (in place), or states that share no buffer but agree in their
+ *               sizes; then every entry of `to` is written and `from` stays as it is, so that a step can be taken back
+ *   want_len [batch] i32, not the seq_len of `to`
+ *   cu_rows  [batch + 1] i32 out: rows cu_rows[b] .. cu_rows[b + 1] - 1 are the new slots of sequence b, ascending
+ *   row_pos  [m_upper] i32 out: the row's slot in its sequence
+ *   row_len  [m_upper] i32 out or null: row_pos + 1 (what a row sees in causal order)
+ *   row_seq  [m_upper] i32 out or null: the row's sequence
+ *   row_slot [m_upper] i64 out or null: the row's slot in the pool, page * page_slots + row_pos % page_slots (-1: no such page)
+ *   workspace   sl_kv8_pages_bytes bytes, 4-byte aligned; needs no initialisation, calls that may overlap in time must not share one
+ * Entries of the row arrays behind cu_rows[batch] are left as they are.  m_upper <= 2^20.  Lengths outside 0 .. max_pages *
+ * page_slots and counts outside 0 .. n_pages are taken as the nearest of these.  Pages are not counted: a page that two sequences
+ * share must not be given up by both.  The results do not depend on timing. */
+int sl_kv8_pages_bytes(int32_t batch, size_t *out);
+int sl_kv8_pages_resize(void *stream, const sl_kv8_pages *from /* host */, const sl_kv8_pages *to /* host */, const int32_t *want_len,
+                        int32_t *cu_rows, int32_t *row_pos, int32_t *row_len, int32_t *row_seq, int64_t *row_slot, int32_t m_upper,
+                        void *workspace, size_t workspace_bytes);
+
+/* Rotary positions.  freqs [rot_dim / 2] f64 holds the frequency of each pair in TURNS (not radians) per slot:
+ *   f_j = theta^(-2 j / rot_dim) / (2 pi), then
+ *   SL_ROPE_PLAIN   as it is
+ *   SL_ROPE_LINEAR  f_j / factor
+ *   SL_ROPE_BASE    with theta factor^(rot_dim / (rot_dim - 2)) for theta (rot_dim >= 4)
+ *   SL_ROPE_TURNS   pairs that turn at least high_turns times in original_len slots as they are, those of at most low_turns divided by
+ *                   factor, between them g f_j + (1 - g) f_j / factor with g = (original_len f_j - low_turns) / (high_turns - low_turns)
+ * sl_rope_freqs writes such a table (8-byte aligned); a caller may also fill one with frequencies of its own.  rot_dim even, 2 .. 1024;
+ * theta and factor positive; for SL_ROPE_TURNS original_len positive and low_turns < high_turns, otherwise they are not looked at. */
+enum { SL_ROPE_PLAIN = 0, SL_ROPE_LINEAR = 1, SL_ROPE_BASE = 2, SL_ROPE_TURNS = 3 };
+int sl_rope_freqs(void *stream, double *freqs, int32_t rot_dim, double theta, int32_t scaling, double factor, double original_len,
+                  double low_turns, double high_turns);
+/* Turn rows of queries, and of keys, to their positions: a pair (a, b) of a head's first rot_dim numbers becomes
+ *   amplitude (a cos t - b sin t),  amplitude (a sin t + b cos t),   t = 2 pi row_pos[r] f_j,
+ * pair j being numbers (j, j + rot_dim / 2), or (2 j, 2 j + 1) if interleaved; numbers from rot_dim on are copied.  A negative
+ * position turns back: the inverse (of amplitude 1), and the gradient.
+ *   q, k     [m_upper] rows of [n_heads or n_kv_heads, d_head] (dtype_in, SL_F32 / SL_BF16), strides in elements (any, at least a row);
+ *            k may be null (then k_out is not looked at)
+ *   q_out, k_out  likewise (dtype_out); each may be its input with the same type and stride (in place), otherwise outputs must not
+ *            overlap inputs or one another
+ *   m_dev    the true number of rows (cu_rows + batch); rows past min(*m_dev, m_upper) are neither read nor written
+ * d_head 2 .. 1024, rot_dim <= d_head, heads * d_head <= 2^20, m_upper <= 2^20.  The angle is formed in fp64 and sine and cosine are
+ * rounded to fp32 once, at any position; the pair is turned in fp32 and rounded to dtype_out once.  Pointers have the alignment of
+ * their type; rows whose pieces are 16-byte aligned are the fast ones. */
+int sl_rope_rows(void *stream, const void *q, int64_t q_stride, void *q_out, int64_t q_out_stride, int32_t n_heads, const void *k,
+                 int64_t k_stride, void *k_out, int64_t k_out_stride, int32_t n_kv_heads, int32_t dtype_in, int32_t dtype_out, int32_t d_head,
+                 int32_t rot_dim, int32_t interleaved, const double *freqs, float amplitude, const int32_t *row_pos,
+                 const int32_t *m_dev, int32_t m_upper);
+
+/* Low-rank adapters beside a projection of k inputs and n outputs: slot a of a bank holds A_a [rank_a, k] and B_a [n, rank_a] (bf16) and a
+ * factor scale_a, and stands for the weights scale_a B_a A_a.  Ranks may differ, up to max_rank.  The struct is a HOST struct. */
+typedef struct sl_adapters {
+  void *bank;                    /* sl_adapters_bytes bytes, 256-byte aligned; its contents are private                 */
+  size_t bank_bytes;
+  int32_t n_slots, max_rank;     /* 1 .. 65536 slots; 1 .. 256                                                          */
+  int32_t n, k;                  /* 1 .. 2^20 each, k a multiple of 8                                                   */
+} sl_adapters;
+int sl_adapters_bytes(int32_t n_slots, int32_t max_rank, int32_t n, int32_t k, size_t *out);
+/* All slots empty (an empty slot adds nothing). */
+int sl_adapters_init(void *stream, const sl_adapters *ad /* host */);
+/* Write slot `slot`: a [rank, k], b [n, rank], row-major, 16- and 2-byte aligned; rank 0 empties the slot (a and b may be null). */
+int sl_adapters_pack(void *stream, const sl_adapters *ad /* host */, int32_t slot, int32_t rank, float scale, const void *a, const void *b);
+/* y[r] = sum_s base[s][r] + scale_a B_a (A_a x[r]) with a = row_adapter[r], for the first min(*m_dev, m_upper) rows.
+ *   x            [m_upper, k] bf16, row-major, 16-byte aligned
+ *   row_adapter  [m_upper] i32; outside 0 .. n_slots - 1: no adapter.  Rows of one adapter share the reading of its weights if they
+ *                stand together
+ *   base         [splits][m_upper][n] fp32: what sl_linear_forward (its k-split planes) or sl_linear_q4_forward left in y_f32; null:
+ *                zeros.  splits 1 .. 64
+ *   y_f32 / y_bf16  [m_upper, n], exactly one; y_f32 may be base with splits = 1, otherwise they must not overlap
+ *   workspace    sl_adapters_workspace_bytes bytes, 256-byte aligned; needs no initialisation, calls that may overlap in time must not
+ *                share one
+ * Rows past the count are neither read nor written, and no row touches another's result.  Products are accumulated in fp32; A x[r] is held in
+ * fp32 and goes into the second product with 24 bits; a result is rounded once.  An A x[r] whose product with scale leaves fp32's range
+ * comes out as NaN or an infinity.  The same sums in the same order in every call of one shape.  m_upper <= 2^16. */
+int sl_adapters_workspace_bytes(const sl_adapters *ad /* host */, int32_t m_upper, size_t *out);
+int sl_adapters_forward(void *stream, const sl_adapters *ad /* host */, const void *x, const int32_t *row_adapter, const int32_t *m_dev,
+                        int32_t m_upper, const float *base, int32_t splits, float *y_f32, void *y_bf16, void *workspace,
+                        size_t workspace_bytes);
+
+/* Draw a token for each row from its filtered posterior, with a uniform number that the caller brings.
+ *   Weights W_v = rint(2^44 exp((z_v - max z) / temperature)) as whole numbers (u has 24 bits: what weighs less than 2^-45 of the largest is
+ *   never drawn); NaN and -infinity are never drawn.  Tokens in descending order of z, ties to the lower id:
+ *     top_k  > 0: the first top_k of them (0 or less: all)
+ *     top_p  < 1: of these the fewest, from the first on, whose weights add up to at least top_p times all of theirs (at least one)
+ *     min_p  > 0: of these the ones with W_v >= min_p 2^44 (at least one)
+ *   token = the lowest id among the kept at which the running sum of kept weights, by ids, exceeds u times their sum.  A temperature that is
+ *   not above 0 keeps the first of the order only.  Sums are exact whole numbers, and products with u and top_p are formed in fp64, so the
+ *   result depends on the row alone.
+ *   logits   [n_rows] rows of vocab numbers (dtype SL_F32 / SL_BF16), row_stride elements apart; vocab 1 .. 2^18
+ *   row_map  [m_upper] i32 or null: row r draws from logits row row_map[r] (a step's active_idx), otherwise from row r.  A row that
+ *            is not in 0 .. n_rows - 1 counts as one without a token to draw
+ *   temperature f32, top_k i32, top_p f32, min_p f32: [m_upper] each, or null: 1, and no filter
+ *   uniform  [m_upper] f32 in [0, 1); taken as the nearest number there, NaN as 0
+ *   token    [m_upper] i32 out; prob [m_upper] f32 out or null: W of the token over the sum of kept W; kept [m_upper] i32 out or null: their number
+ *   workspace  sl_sample_filtered_bytes bytes, 256-byte aligned; needs no initialisation, calls that may overlap in time must not
+ *            share one
+ * A row without a token to draw gets token 0, prob 0 and kept 0.  Rows past min(*m_dev, m_upper) are neither read nor written; m_upper <= 2^20. */
+int sl_sample_filtered_bytes(int32_t m_upper, int32_t vocab, size_t *out);
+int sl_sample_filtered(void *stream, const void *logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                       const int32_t *row_map, const int32_t *m_dev, int32_t m_upper, const float *temperature, const int32_t *top_k,
+                       const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob, int32_t *kept,
+                       void *workspace, size_t workspace_bytes);
+
 /* ---- measurement support ------------------------------------------------------------
  * Per-kernel timing of the step's launches with HIP events on the step's own stream.
  * Between sl_profile_begin and sl_profile_end every kernel the library launches for this

@@ -38,6 +38,15 @@ class sl_kv8(C.Structure):
                 ("max_pages", C.c_int32)]
 
 
+class sl_kv8_pages(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("seq_len", C.c_void_p), ("free_pages", C.c_void_p), ("n_free", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_slots", C.c_int32), ("batch", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class sl_adapters(C.Structure):
+    _fields_ = [("bank", C.c_void_p), ("bank_bytes", C.c_size_t), ("n_slots", C.c_int32), ("max_rank", C.c_int32), ("n", C.c_int32), ("k", C.c_int32)]
+
+
 _P, _I, _Z, _L = C.c_void_p, C.c_int32, C.c_size_t, C.c_int64
 _SIGS = {
     "sl_init": [C.POINTER(sl_config), C.POINTER(_P)],
@@ -81,6 +90,18 @@ _SIGS = {
     "sl_kv8_read": [_P, C.POINTER(sl_kv8), _P, _P, _I, _L, _L, _P, _P, _I],
     "sl_kv8_attention_bytes": [C.POINTER(sl_kv8), _I, _I, _I, C.POINTER(_Z)],
     "sl_kv8_attention": [_P, C.POINTER(sl_kv8), _P, _I, _L, _I, _P, _P, _P, _I, _I, C.c_float, _P, _L, _P, _Z],
+    "sl_kv8_pages_init": [_P, C.POINTER(sl_kv8_pages)],
+    "sl_kv8_pages_bytes": [_I, C.POINTER(_Z)],
+    "sl_kv8_pages_resize": [_P, C.POINTER(sl_kv8_pages), C.POINTER(sl_kv8_pages), _P, _P, _P, _P, _P, _P, _I, _P, _Z],
+    "sl_rope_freqs": [_P, _P, _I, C.c_double, _I, C.c_double, C.c_double, C.c_double, C.c_double],
+    "sl_rope_rows": [_P, _P, _L, _P, _L, _I, _P, _L, _P, _L, _I, _I, _I, _I, _I, _I, _P, C.c_float, _P, _P, _I],
+    "sl_adapters_bytes": [_I, _I, _I, _I, C.POINTER(_Z)],
+    "sl_adapters_init": [_P, C.POINTER(sl_adapters)],
+    "sl_adapters_pack": [_P, C.POINTER(sl_adapters), _I, _I, C.c_float, _P, _P],
+    "sl_adapters_workspace_bytes": [C.POINTER(sl_adapters), _I, C.POINTER(_Z)],
+    "sl_adapters_forward": [_P, C.POINTER(sl_adapters), _P, _P, _P, _I, _P, _I, _P, _P, _P, _Z],
+    "sl_sample_filtered_bytes": [_I, _I, C.POINTER(_Z)],
+    "sl_sample_filtered": [_P, _P, _I, _L, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _Z],
     "sl_peak_probe_mfma": [_P, _P, _Z, _I, _I, _P, _Z, C.POINTER(C.c_int64)],
     "sl_peak_probe_stream": [_P, _P, _P, _Z, _P, _Z],
     "sl_profile_begin": [_P, _I],
@@ -528,6 +549,179 @@ def sl_kv8_attention(kv, q, cu_rows, seq_len, m_upper, len_upper, scale, out, wo
                                     _addr(workspace, _U8, dev), workspace.numel())
     if status:
         raise SureLockError("sl_kv8_attention", status)
+
+
+# ---- pages of the cache ------------------------------------------------------------------------
+_I64, _F64 = torch.int64, torch.float64
+
+
+class KV8Pages:
+    """Owns what hands out the pages of a paged cache: page_table [batch, max_pages], seq_len [batch], free_pages [n_pages] and n_free [1] (int32,
+    device), and the workspace of its resizing.  page_table is what KV8 takes, for the caches of all layers.  Every page starts free."""
+
+    def __init__(self, n_pages, page_slots, batch, max_pages, device="cuda:0"):
+        with torch.cuda.device(device):
+            new = lambda *shape: torch.empty(*shape, dtype=_I32, device=device)  # noqa: E731
+            self.n_pages, self.page_slots, self.batch, self.max_pages = n_pages, page_slots, batch, max_pages
+            self.workspace = torch.empty(sl_kv8_pages_bytes(batch), dtype=_U8, device=device)
+            self.page_table, self.seq_len, self.free_pages, self.n_free = new(batch, max_pages), new(batch), new(n_pages), new(1)
+            self.device = self.page_table.get_device()
+            self.desc = sl_kv8_pages(*(t.data_ptr() for t in (self.page_table, self.seq_len, self.free_pages, self.n_free)), n_pages, page_slots, batch,
+                                     max_pages)
+            self.desc_ref = C.byref(self.desc)
+            sl_kv8_pages_init(self)
+
+
+def sl_kv8_pages_bytes(batch):
+    out = _Z()
+    _check("sl_kv8_pages_bytes", lib().sl_kv8_pages_bytes(batch, C.byref(out)))
+    return out.value
+
+
+def sl_kv8_pages_init(pages):
+    dev, stream = _kv8_here(pages)
+    _check("sl_kv8_pages_init", lib().sl_kv8_pages_init(stream, pages.desc_ref))
+
+
+def sl_kv8_pages_resize(pages, want_len, cu_rows, row_pos, m_upper, to=None, row_len=None, row_seq=None, row_slot=None):
+    """pages (and to, unless the step is taken in place): KV8Pages; row_slot int64, everything else int32 (see the header)."""
+    _require_gpu(want_len)
+    to = pages if to is None else to
+    dev, stream = _kv8_here(pages)
+    if to.device != dev:
+        raise ValueError(f"the state to write is on cuda:{to.device}, the current device is cuda:{dev}")
+    status = lib().sl_kv8_pages_resize(stream, pages.desc_ref, to.desc_ref, _addr(want_len, _I32, dev, pages.batch), _addr(cu_rows, _I32, dev, pages.batch + 1),
+                                       _addr(row_pos, _I32, dev, m_upper), None if row_len is None else _addr(row_len, _I32, dev, m_upper),
+                                       None if row_seq is None else _addr(row_seq, _I32, dev, m_upper),
+                                       None if row_slot is None else _addr(row_slot, _I64, dev, m_upper), m_upper, to.workspace.data_ptr(),
+                                       to.workspace.numel())
+    if status:
+        raise SureLockError("sl_kv8_pages_resize", status)
+
+
+# ---- rotary positions ------------------------------------------------------------------------
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3}
+
+
+def sl_rope_freqs(freqs, theta, scaling="plain", factor=1.0, original_len=0.0, low_turns=0.0, high_turns=0.0):
+    """freqs [rot_dim / 2] float64, written; scaling: one of ROPE_SCALINGS."""
+    _require_gpu(freqs)
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling is one of {', '.join(ROPE_SCALINGS)}, not {scaling!r}")
+    dev, stream = _here()
+    _check("sl_rope_freqs", lib().sl_rope_freqs(stream, _addr(freqs, _F64, dev), 2 * freqs.numel(), theta, ROPE_SCALINGS[scaling], factor, original_len,
+                                                low_turns, high_turns))
+
+
+def sl_rope_rows(q, q_out, k, k_out, freqs, row_pos, m_dev, m_upper, interleaved=False, amplitude=1.0):
+    """q, k and what comes out: rows [*, heads, d_head] that may lie apart; k and k_out may be None.  rot_dim is 2 freqs.numel()."""
+    _require_gpu(q)
+    if m_upper == 0:
+        return
+    dev, stream = _here()
+    t_in, t_out, heads, d = q.dtype, q_out.dtype, q.shape[1], q.shape[2]
+    (qp, qs), (qo, qos) = _head_rows(q, t_in, dev, heads, d, m_upper), _head_rows(q_out, t_out, dev, heads, d, m_upper)
+    kp = ks = ko = kos = None
+    kv_heads = 0
+    if k is not None:
+        kv_heads = k.shape[1]
+        (kp, ks), (ko, kos) = _head_rows(k, t_in, dev, kv_heads, d, m_upper), _head_rows(k_out, t_out, dev, kv_heads, d, m_upper)
+    status = lib().sl_rope_rows(stream, qp, qs, qo, qos, heads, kp, ks or 0, ko, kos or 0, kv_heads, _float_code(q), _float_code(q_out), d, 2 * freqs.numel(),
+                                int(interleaved), _addr(freqs, _F64, dev), amplitude, _addr(row_pos, _I32, dev, m_upper), _addr(m_dev, _I32, dev, 1), m_upper)
+    if status:
+        raise SureLockError("sl_rope_rows", status)
+
+
+# ---- low-rank adapters -----------------------------------------------------------------------
+class Adapters:
+    """Owns a bank of n_slots low-rank adapters, of ranks up to max_rank, beside a projection of k inputs and n outputs.  All slots start empty."""
+
+    def __init__(self, n_slots, max_rank, n, k, device="cuda:0"):
+        with torch.cuda.device(device):
+            self.n_slots, self.max_rank, self.n, self.k = n_slots, max_rank, n, k
+            self.bank = torch.empty(sl_adapters_bytes(n_slots, max_rank, n, k), dtype=_U8, device=device)
+            self.device = self.bank.get_device()
+            self.desc = sl_adapters(self.bank.data_ptr(), self.bank.numel(), n_slots, max_rank, n, k)
+            self.desc_ref = C.byref(self.desc)
+            _check("sl_adapters_init", lib().sl_adapters_init(_stream(), self.desc_ref))
+
+
+def sl_adapters_bytes(n_slots, max_rank, n, k):
+    out = _Z()
+    _check("sl_adapters_bytes", lib().sl_adapters_bytes(n_slots, max_rank, n, k, C.byref(out)))
+    return out.value
+
+
+def sl_adapters_init(ad):
+    dev, stream = _adapters_here(ad)
+    _check("sl_adapters_init", lib().sl_adapters_init(stream, ad.desc_ref))
+
+
+def _adapters_here(ad):
+    dev, stream = _here()
+    if ad.device != dev:
+        raise ValueError(f"the adapters are on cuda:{ad.device}, the current device is cuda:{dev}")
+    return dev, stream
+
+
+def sl_adapters_pack(ad, slot, a, b, scale=1.0):
+    """a [rank, k], b [n, rank] (bfloat16); None for both empties the slot."""
+    dev, stream = _adapters_here(ad)
+    rank = 0
+    if a is not None:
+        rank = a.shape[0]
+        if tuple(a.shape) != (rank, ad.k) or tuple(b.shape) != (ad.n, rank):
+            raise ValueError(f"a [rank, {ad.k}] and b [{ad.n}, rank] are needed, not {tuple(a.shape)} and {tuple(b.shape)}")
+    _check("sl_adapters_pack", lib().sl_adapters_pack(stream, ad.desc_ref, slot, rank, scale, _addr(a, _BF16, dev), None if a is None else _addr(b, _BF16, dev)))
+
+
+def sl_adapters_workspace_bytes(ad, m_upper):
+    out = _Z()
+    _check("sl_adapters_workspace_bytes", lib().sl_adapters_workspace_bytes(ad.desc_ref, m_upper, C.byref(out)))
+    return out.value
+
+
+def sl_adapters_forward(ad, x, row_adapter, m_dev, m_upper, workspace, base=None, splits=1, y_f32=None, y_bf16=None):
+    """x [m_upper, k] bfloat16, row_adapter [m_upper] int32, base [splits, m_upper, n] float32 or None, y_f32 or y_bf16 [m_upper, n]."""
+    _require_gpu(x)
+    if m_upper == 0:
+        return
+    dev, stream = _adapters_here(ad)
+    size = m_upper * ad.n
+    status = lib().sl_adapters_forward(stream, ad.desc_ref, _addr(x, _BF16, dev, m_upper * ad.k), _addr(row_adapter, _I32, dev, m_upper), _addr(m_dev, _I32, dev, 1),
+                                       m_upper, None if base is None else _addr(base, _F32, dev, splits * size), splits,
+                                       None if y_f32 is None else _addr(y_f32, _F32, dev, size), None if y_bf16 is None else _addr(y_bf16, _BF16, dev, size),
+                                       _addr(workspace, _U8, dev), workspace.numel())
+    if status:
+        raise SureLockError("sl_adapters_forward", status)
+
+
+# ---- draws from a filtered posterior ---------------------------------------------------------
+def sl_sample_filtered_bytes(m_upper, vocab):
+    out = _Z()
+    _check("sl_sample_filtered_bytes", lib().sl_sample_filtered_bytes(m_upper, vocab, C.byref(out)))
+    return out.value
+
+
+def sl_sample_filtered(logits, m_dev, m_upper, uniform, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, row_map=None, prob=None,
+                       kept=None):
+    """logits: rows [*, vocab] that may lie apart (float32 or bfloat16); one entry for each of m_upper rows in everything else, int32 for top_k, row_map,
+    token and kept, float32 for the others."""
+    _require_gpu(logits)
+    if m_upper == 0:
+        return
+    dev, stream = _here()
+    rows, vocab = logits.shape
+    code = _float_code(logits)
+    if logits.get_device() != dev or (logits.stride(1) != 1 and vocab > 1) or (row_map is None and rows < m_upper):
+        raise ValueError(f"at least {m_upper} rows of logits on cuda:{dev} are needed, each of them dense, not {tuple(logits.shape)}, strides {logits.stride()}, "
+                         f"on {logits.device}")
+    opt = lambda t, dtype: None if t is None else _addr(t, dtype, dev, m_upper)  # noqa: E731
+    status = lib().sl_sample_filtered(stream, logits.data_ptr(), code, logits.stride(0) if rows > 1 else vocab, rows, vocab, opt(row_map, _I32), _addr(m_dev, _I32, dev, 1),
+                                      m_upper, opt(temperature, _F32), opt(top_k, _I32), opt(top_p, _F32), opt(min_p, _F32), _addr(uniform, _F32, dev, m_upper),
+                                      _addr(token, _I32, dev, m_upper), opt(prob, _F32), opt(kept, _I32), _addr(workspace, _U8, dev), workspace.numel())
+    if status:
+        raise SureLockError("sl_sample_filtered", status)
 
 
 def sl_peak_probe_mfma(operands, iters, waves_per_simd, sink):

@@ -827,3 +827,141 @@ extern "C" int sl_kv8_attention(void* stream, const sl_kv8* kv, const void* q, i
   return slk_kv8_attention((hipStream_t)stream, v, kv->d_head, dtype, q, q_stride, n_heads, cu_rows, seq_len, row_len, m_upper, len_upper,
                            scale, out, out_stride, workspace);
 }
+
+// ---- pages of the cache --------------------------------------------------------------------------------
+static bool kv8_pages_ok(const sl_kv8_pages* p) {
+  if (!p || !p->page_table || !p->seq_len || !p->free_pages || !p->n_free) return false;
+  if (((uintptr_t)p->page_table | (uintptr_t)p->seq_len | (uintptr_t)p->free_pages | (uintptr_t)p->n_free) % 4) return false;
+  const int32_t ps = p->page_slots;
+  if (!(ps == 16 || ps == 32 || ps == 64 || ps == 128 || ps == 256)) return false;
+  if (p->n_pages < 1 || p->n_pages > 1 << 30 || p->batch < 1 || p->batch > SL_MAX_BATCH || p->max_pages < 1) return false;
+  return (int64_t)p->max_pages * ps <= (int64_t)1 << 30 && (int64_t)p->max_pages * p->batch <= (int64_t)1 << 30;
+}
+
+extern "C" int sl_kv8_pages_init(void* stream, const sl_kv8_pages* pages) {
+  if (!kv8_pages_ok(pages)) return SL_EINVAL;
+  return slk_kv8_pages_init((hipStream_t)stream, pages);
+}
+
+extern "C" int sl_kv8_pages_bytes(int32_t batch, size_t* out) {
+  if (!out || batch < 1 || batch > SL_MAX_BATCH) return SL_EINVAL;
+  *out = slk_kv8_pages_bytes(batch);
+  return SL_OK;
+}
+
+extern "C" int sl_kv8_pages_resize(void* stream, const sl_kv8_pages* from, const sl_kv8_pages* to, const int32_t* want_len, int32_t* cu_rows,
+                                   int32_t* row_pos, int32_t* row_len, int32_t* row_seq, int64_t* row_slot, int32_t m_upper, void* workspace,
+                                   size_t workspace_bytes) {
+  if (!kv8_pages_ok(from) || !kv8_pages_ok(to)) return SL_EINVAL;
+  if (from->n_pages != to->n_pages || from->page_slots != to->page_slots || from->batch != to->batch || from->max_pages != to->max_pages) return SL_EINVAL;
+  const int same = (from->page_table == to->page_table) + (from->seq_len == to->seq_len) + (from->free_pages == to->free_pages) + (from->n_free == to->n_free);
+  if (same != 0 && same != 4) return SL_EINVAL;
+  if (!want_len || !cu_rows || want_len == to->seq_len || m_upper < 0 || m_upper > 1 << 20 || (m_upper > 0 && !row_pos)) return SL_EINVAL;
+  if (((uintptr_t)want_len | (uintptr_t)cu_rows | (uintptr_t)row_pos | (uintptr_t)row_len | (uintptr_t)row_seq) % 4 || (uintptr_t)row_slot % 8) return SL_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 4) return SL_EINVAL;
+  if (workspace_bytes < slk_kv8_pages_bytes(from->batch)) return SL_ENOSPC;
+  return slk_kv8_pages_resize((hipStream_t)stream, from, to, want_len, cu_rows, row_pos, row_len, row_seq, row_slot, m_upper, workspace);
+}
+
+// ---- rotary positions ------------------------------------------------------------------------------------
+extern "C" int sl_rope_freqs(void* stream, double* freqs, int32_t rot_dim, double theta, int32_t scaling, double factor, double original_len,
+                             double low_turns, double high_turns) {
+  if (!freqs || (uintptr_t)freqs % 8 || rot_dim < 2 || rot_dim > 1024 || rot_dim % 2) return SL_EINVAL;
+  if (!(theta > 0) || !(theta < __builtin_inf()) || !(factor > 0) || !(factor < __builtin_inf())) return SL_EINVAL;
+  if (scaling < SL_ROPE_PLAIN || scaling > SL_ROPE_TURNS || (scaling == SL_ROPE_BASE && rot_dim < 4)) return SL_EINVAL;
+  if (scaling == SL_ROPE_TURNS && (!(original_len > 0) || !(original_len < __builtin_inf()) || !(low_turns < high_turns) ||
+                                   !(low_turns > -__builtin_inf()) || !(high_turns < __builtin_inf()))) return SL_EINVAL;
+  return slk_rope_freqs((hipStream_t)stream, freqs, rot_dim, theta, scaling, factor, original_len, low_turns, high_turns);
+}
+
+static bool rope_side_ok(const void* in, int64_t in_stride, const void* out, int64_t out_stride, int32_t heads, int32_t d, int32_t ti, int32_t to) {
+  const int64_t width = (int64_t)heads * d, most = (int64_t)1 << 40;
+  if (!in || !out || heads < 1 || width > 1 << 20 || in_stride < width || out_stride < width || in_stride > most || out_stride > most) return false;
+  if ((uintptr_t)in % sl_tsize(ti) || (uintptr_t)out % sl_tsize(to)) return false;
+  return in != out || (in_stride == out_stride && ti == to);
+}
+
+extern "C" int sl_rope_rows(void* stream, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t n_heads, const void* k,
+                            int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t n_kv_heads, int32_t dtype_in, int32_t dtype_out,
+                            int32_t d_head, int32_t rot_dim, int32_t interleaved, const double* freqs, float amplitude, const int32_t* row_pos,
+                            const int32_t* m_dev, int32_t m_upper) {
+  if ((dtype_in != SL_F32 && dtype_in != SL_BF16) || (dtype_out != SL_F32 && dtype_out != SL_BF16)) return SL_EINVAL;
+  if (d_head < 2 || d_head > 1024 || rot_dim < 2 || rot_dim > d_head || rot_dim % 2 || m_upper < 0 || m_upper > 1 << 20) return SL_EINVAL;
+  if (!freqs || !row_pos || !m_dev || (uintptr_t)freqs % 8 || ((uintptr_t)row_pos | (uintptr_t)m_dev) % 4) return SL_EINVAL;
+  if (!rope_side_ok(q, q_stride, q_out, q_out_stride, n_heads, d_head, dtype_in, dtype_out)) return SL_EINVAL;
+  if (k && (!rope_side_ok(k, k_stride, k_out, k_out_stride, n_kv_heads, d_head, dtype_in, dtype_out) || q_out == k_out)) return SL_EINVAL;
+  if (m_upper == 0) return SL_OK;
+  return slk_rope_rows((hipStream_t)stream, q, q_stride, q_out, q_out_stride, n_heads, k, k_stride, k_out, k_out_stride, n_kv_heads, dtype_in, dtype_out,
+                       d_head, rot_dim, interleaved != 0, freqs, amplitude, row_pos, m_dev, m_upper);
+}
+
+// ---- low-rank adapters -----------------------------------------------------------------------------------
+static bool adapters_shape_ok(int32_t n_slots, int32_t max_rank, int32_t n, int32_t k) {
+  return n_slots >= 1 && n_slots <= 1 << 16 && max_rank >= 1 && max_rank <= 256 && n >= 1 && n <= 1 << 20 && k >= 8 && k <= 1 << 20 && k % 8 == 0;
+}
+
+extern "C" int sl_adapters_bytes(int32_t n_slots, int32_t max_rank, int32_t n, int32_t k, size_t* out) {
+  if (!out || !adapters_shape_ok(n_slots, max_rank, n, k)) return SL_EINVAL;
+  const sl_adapters ad{nullptr, 0, n_slots, max_rank, n, k};
+  *out = slk_adapters_bytes(&ad);
+  return SL_OK;
+}
+
+static int adapters_check(const sl_adapters* ad) {
+  if (!ad || !ad->bank || (uintptr_t)ad->bank % 256 || !adapters_shape_ok(ad->n_slots, ad->max_rank, ad->n, ad->k)) return SL_EINVAL;
+  return ad->bank_bytes < slk_adapters_bytes(ad) ? SL_ENOSPC : SL_OK;
+}
+
+extern "C" int sl_adapters_init(void* stream, const sl_adapters* ad) {
+  SL_TRY(adapters_check(ad));
+  return slk_adapters_init((hipStream_t)stream, ad);
+}
+
+extern "C" int sl_adapters_pack(void* stream, const sl_adapters* ad, int32_t slot, int32_t rank, float scale, const void* a, const void* b) {
+  SL_TRY(adapters_check(ad));
+  if (slot < 0 || slot >= ad->n_slots || rank < 0 || rank > ad->max_rank) return SL_EINVAL;
+  if (rank > 0 && (!a || !b || (uintptr_t)a % 16 || (uintptr_t)b % 2)) return SL_EINVAL;
+  return slk_adapters_pack((hipStream_t)stream, ad, slot, rank, scale, a, b);
+}
+
+extern "C" int sl_adapters_workspace_bytes(const sl_adapters* ad, int32_t m_upper, size_t* out) {
+  if (!ad || !out || !adapters_shape_ok(ad->n_slots, ad->max_rank, ad->n, ad->k) || m_upper < 0 || m_upper > 1 << 16) return SL_EINVAL;
+  *out = slk_adapters_workspace_bytes(ad, m_upper);
+  return SL_OK;
+}
+
+extern "C" int sl_adapters_forward(void* stream, const sl_adapters* ad, const void* x, const int32_t* row_adapter, const int32_t* m_dev, int32_t m_upper,
+                                   const float* base, int32_t splits, float* y_f32, void* y_bf16, void* workspace, size_t workspace_bytes) {
+  SL_TRY(adapters_check(ad));
+  if (!x || !row_adapter || !m_dev || (uintptr_t)x % 16 || ((uintptr_t)row_adapter | (uintptr_t)m_dev) % 4) return SL_EINVAL;
+  if (m_upper < 0 || m_upper > 1 << 16 || splits < 1 || splits > 64 || !y_f32 == !y_bf16) return SL_EINVAL;
+  if ((uintptr_t)base % 4 || (uintptr_t)y_f32 % 4 || (uintptr_t)y_bf16 % 2) return SL_EINVAL;
+  if (base && ((const void*)base == y_bf16 || (base == y_f32 && splits != 1))) return SL_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 256) return SL_EINVAL;
+  if (m_upper == 0) return SL_OK;
+  if (workspace_bytes < slk_adapters_workspace_bytes(ad, m_upper)) return SL_ENOSPC;
+  return slk_adapters_forward((hipStream_t)stream, ad, x, row_adapter, m_dev, m_upper, base, splits, y_f32, y_bf16, workspace);
+}
+
+// ---- draws from a filtered posterior -----------------------------------------------------------------------
+extern "C" int sl_sample_filtered_bytes(int32_t m_upper, int32_t vocab, size_t* out) {
+  if (!out || m_upper < 0 || m_upper > 1 << 20 || vocab < 1 || vocab > 1 << 18) return SL_EINVAL;
+  *out = slk_sample_filtered_bytes(m_upper, vocab);
+  return SL_OK;
+}
+
+extern "C" int sl_sample_filtered(void* stream, const void* logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,
+                                  const int32_t* row_map, const int32_t* m_dev, int32_t m_upper, const float* temperature, const int32_t* top_k,
+                                  const float* top_p, const float* min_p, const float* uniform, int32_t* token, float* prob, int32_t* kept,
+                                  void* workspace, size_t workspace_bytes) {
+  if (!logits || !m_dev || !uniform || !token || (dtype != SL_F32 && dtype != SL_BF16) || (uintptr_t)logits % sl_tsize(dtype)) return SL_EINVAL;
+  if (vocab < 1 || vocab > 1 << 18 || n_rows < 1 || m_upper < 0 || m_upper > 1 << 20) return SL_EINVAL;
+  if (row_stride < vocab || row_stride > (int64_t)1 << 40) return SL_EINVAL;
+  if (((uintptr_t)row_map | (uintptr_t)m_dev | (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)uniform |
+       (uintptr_t)token | (uintptr_t)prob | (uintptr_t)kept) % 4) return SL_EINVAL;
+  if (!workspace || (uintptr_t)workspace % 256) return SL_EINVAL;
+  if (m_upper == 0) return SL_OK;
+  if (workspace_bytes < slk_sample_filtered_bytes(m_upper, vocab)) return SL_ENOSPC;
+  return slk_sample_filtered((hipStream_t)stream, logits, dtype, row_stride, n_rows, vocab, row_map, m_dev, m_upper, temperature, top_k, top_p, min_p,
+                             uniform, token, prob, kept, workspace);
+}

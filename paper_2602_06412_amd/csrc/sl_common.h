@@ -372,6 +372,29 @@ int slk_q4_quantize(hipStream_t s, const void* w, int dtype, int n, int k, int g
 int slk_q4_pack(hipStream_t s, const void* codes, const void* scales, const void* zeros, int n, int k, int group, void* packed);
 int slk_q4_linear(hipStream_t s, const void* x, const void* packed, const int32_t* m_dev, int m_upper, int n, int k, int group, float* y_f32,
                   void* y_bf16, const int32_t* row_map);
+// kv8_pages.hip: pages of the 8-bit cache from the lengths that sequences want
+size_t slk_kv8_pages_bytes(int batch);
+int slk_kv8_pages_init(hipStream_t s, const sl_kv8_pages* p);
+int slk_kv8_pages_resize(hipStream_t s, const sl_kv8_pages* from, const sl_kv8_pages* to, const int32_t* want_len, int32_t* cu_rows, int32_t* row_pos,
+                         int32_t* row_len, int32_t* row_seq, int64_t* row_slot, int m_upper, void* workspace);
+// rope.hip: rotary positions as a call of its own
+int slk_rope_freqs(hipStream_t s, double* freqs, int rot, double theta, int scaling, double factor, double original_len, double low_turns,
+                   double high_turns);
+int slk_rope_rows(hipStream_t s, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, int n_heads, const void* k, int64_t k_stride,
+                  void* k_out, int64_t k_out_stride, int n_kv_heads, int dtype_in, int dtype_out, int d, int rot, int pairs, const double* freqs,
+                  float amplitude, const int32_t* row_pos, const int32_t* m_dev, int m_upper);
+// adapters.hip: low-rank adapters beside a projection
+size_t slk_adapters_bytes(const sl_adapters* ad);
+int slk_adapters_init(hipStream_t s, const sl_adapters* ad);
+int slk_adapters_pack(hipStream_t s, const sl_adapters* ad, int slot, int rank, float scale, const void* a, const void* b);
+size_t slk_adapters_workspace_bytes(const sl_adapters* ad, int m_upper);
+int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
+                         const float* base, int splits, float* y_f32, void* y_bf16, void* workspace);
+// sample_filtered.hip: draws from a filtered posterior
+size_t slk_sample_filtered_bytes(int m_upper, int vocab);
+int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t row_stride, int n_rows, int vocab, const int32_t* row_map,
+                        const int32_t* m_dev, int m_upper, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                        const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace);
 // attention_mfma.hip
 int slk_attention_mfma(hipStream_t s, const void* q, const void* kc, const void* vc, const int32_t* active_idx,
                        const int32_t* m_dev, int m_upper, int B, int H, int N, int n_pad, void* o, float* scratch);
