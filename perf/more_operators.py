@@ -283,7 +283,7 @@ def prepare(case, seed):
         st["m"] = _ints([c["rows"]])
         if own:
             st["freqs"] = torch.empty(c["rot"] // 2, dtype=torch.float64, device=DEV)
-            B.sl_rope_freqs(st["freqs"], ROPE["theta"], **({} if c["scaling"] == "plain" else dict(ROPE, theta=ROPE["theta"], scaling=c["scaling"])))
+            B.sl_rope_freqs(st["freqs"], **({"theta": ROPE["theta"]} if c["scaling"] == "plain" else dict(ROPE, scaling=c["scaling"])))
             st["q_out"], st["k_out"] = (torch.empty(t.shape, dtype=_dtype(c["out"]), device=DEV) for t in (st["q"], st["k"]))
         else:
             st["freqs"] = _freqs(c)
