@@ -1,25 +1,63 @@
 // A token for each row from its filtered posterior, with a given uniform number.
 //
-// Every filter keeps a beginning of the row's order (z descending, id ascending), so what is kept is a threshold: the key of the last
-// kept z and, among the tokens of that very z, the last kept id.  Weights are whole numbers, W = rint(2^44 exp((z - max) / T)): at most
-// 2^18 of them add up to less than 2^63, in any order and from any thread, to the same sum.
+// Every filter keeps a beginning of the row's order (z descending, id ascending), so what is kept is a border: all tokens above one number
+// and, in order of ids, some of those that equal it.  Weights are whole numbers, W = rint(2^44 exp((z - max) / T)): at most 2^18 of them
+// add up to less than 2^63, in any order and from any thread, to the same sum.
+//
+// A workgroup takes a row and passes over it as often as it has to, 64 bytes a thread in flight.
+//
+// Weights.  2^t = 2^n T[i] 2^(r / 256) with 256 t = 256 n + i + r, |r| <= 1 / 2: a table of 256 powers and a sum of four terms, off by
+// less than 2^-51 of itself.
+// bf16.  A weight depends on 16 bits, and logits take a few thousand of the 65536 numbers.  These are counted one by one (LDS, an atomic
+// add of one a token): order, sums of weights and borders follow from counts times weights, 64 numbers a wave and step, and the exponential is
+// taken once for each number that occurs; the last pass reads the weights of what is kept from a table.  Numbers below 2^-10 in size, nearly
+// half of the 65536 and hardly any logit, share one bin and are weighed token by token.
+// fp32, and bf16 where that does not do (a border among the tiny numbers, a temperature in the hundreds): the border's key in three
+// steps of 11, 11 and 10 bits, each a pass that adds up weights (or counts) for each value of the digit.
 #include "sl_common.h"
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kBins = 6144, kGroups = kBins / 64, kDigits = 2048;
+constexpr int kTiny = 0x3a80;                             // rank of 2^-10
+constexpr int kMaxParts = 1024;                           // 64 times 16 bytes of 1024 threads: 2^18 fp32 numbers
 constexpr double kUnit = 17592186044416.0;                // 2^44
 
 struct SampleArgs {
   const void* logits;
   int64_t row_stride;
-  int n_rows, vocab, m_upper;
+  int n_rows, vocab, m_upper, wide;                       // wide: every row is 16-byte aligned
   const int32_t *row_map, *m_dev, *top_k;
   const float *temperature, *top_p, *min_p, *uniform;
   int32_t* token;
   float* prob;
   int32_t* kept;
 };
+
+struct Shared {
+  union {
+    uint32_t counts[kBins + 4];                           // (the last: what is beyond the bins)
+    uint64_t weights[kBins + 4];
+    uint64_t digits[kDigits];
+  };
+  union {
+    struct {
+      uint64_t mass[kGroups];
+      uint32_t count[kGroups];
+    } group;
+    struct {                                              // of a wave's part of a piece, in order of ids
+      uint64_t sum[kMaxParts];
+      uint32_t ties[kMaxParts];
+    } part;
+  };
+  double powers[256];
+  uint64_t sums[16], sums2[16];
+  uint64_t found, found2;
+  uint32_t word;
+  int index;
+  float most[16];
+};
+static_assert(sizeof(Shared) <= 80 * 1024, "two workgroups a CU");
 
 // fp32 as a number whose order is that of z (both zeros alike)
 __device__ inline uint32_t key_of(float z) {
@@ -30,178 +68,489 @@ __device__ inline float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31
 // a token that may be drawn: neither NaN nor -infinity
 __device__ inline bool allowed(float z) { return z > -__builtin_inff(); }
 
-__device__ inline uint64_t weight_of(float z, float most, double heat) {
-  if (z == most) return (uint64_t)kUnit;                  // (an infinity, too)
-  return most < __builtin_inff() ? (uint64_t)rint(exp(((double)z - (double)most) / heat) * kUnit) : 0;
+// Two bf16 numbers as 16-bit integers whose order is that of the numbers, both zeros alike; above +infinity's and below -infinity's are NaNs.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline s16x2 ranks_of(uint32_t w) {
+  const s16x2 x = __builtin_bit_cast(s16x2, w), sign = x >> 15;
+  return (x ^ (sign & (short)0x7fff)) - sign;
 }
+__device__ inline int rank_of(float z) {
+  const uint32_t bits = __float_as_uint(z) >> 16;
+  return bits >> 15 ? -(int)(bits & 0x7fff) : (int)bits;
+}
+__device__ inline float of_rank(int r) { return __uint_as_float((uint32_t)(r < 0 ? 0x8000 - r : r) << 16); }
 
-struct Shared {
-  uint64_t bins[256];
-  uint64_t sums[kWaves];
-  uint64_t found;
-  uint32_t word;
-  int index;
+struct Weigher {
+  double most, rate;                                      // rate: 256 log2(e) / temperature
+  const double* powers;
+  __device__ uint64_t operator()(float z) const {
+    constexpr double kRound = 6755399441055744.0, L = 0.0027076061740622863;      // 1.5 2^52; ln 2 / 256
+    if ((double)z == most) return (uint64_t)kUnit;        // (an infinity, too)
+    const double t = fmax(((double)z - most) * rate, -16384.0), y = t + kRound, r = (t - (y - kRound)) * L;
+    const int n = (int)(uint32_t)__double_as_longlong(y);
+    const double p = fma(r, fma(r, fma(r, fma(r, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0) * powers[n & 255];
+    return (uint64_t)__double_as_longlong(ldexp(p, 44 + (n >> 8)) + 4503599627370496.0) & 0xfffffffffffffull;
+  }
 };
 
+// ---- sums over lanes, by moving lanes ----
+template <int CTRL, int ROWS>
+__device__ inline uint64_t moved(uint64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 15, true), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 15, true);
+  return (uint64_t)hi << 32 | lo;
+}
+// of this lane and those before it
+__device__ inline uint64_t wave_scan(uint64_t v) {
+  v += moved<0x111, 15>(v);                               // within 16 lanes, from 1, 2, 4 and 8 below
+  v += moved<0x112, 15>(v);
+  v += moved<0x114, 15>(v);
+  v += moved<0x118, 15>(v);
+  v += moved<0x142, 10>(v);                               // the first and third sixteen's last lane to the one behind
+  v += moved<0x143, 12>(v);                               // lane 31 to the upper half
+  return v;
+}
+__device__ inline uint64_t lane_of(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+__device__ inline uint64_t wave_total(uint64_t v) { return lane_of(wave_scan(v), 63); }
+
 // sum over the block of the threads before this one; `whole` gets the sum of all
+template <int NT>
 __device__ inline uint64_t before_me(uint64_t v, Shared& sh, uint64_t& whole) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t sum = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t below = __shfl_up((unsigned long long)sum, o, 64);
-    if (lane >= o) sum += below;
-  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t sum = wave_scan(v);
   __syncthreads();
   if (lane == 63) sh.sums[wave] = sum;
   __syncthreads();
-  uint64_t at = 0;
-  whole = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) at += sh.sums[w];
-    whole += sh.sums[w];
-  }
-  return at + sum - v;
+  const uint64_t waves = wave_scan(lane < NT / 64 ? sh.sums[lane] : 0);
+  whole = lane_of(waves, NT / 64 - 1);
+  return (wave ? lane_of(waves, wave - 1) : 0) + sum - v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_filtered_kernel(SampleArgs a) {
-  __shared__ Shared sh;
-  const int r = blockIdx.x, tid = threadIdx.x, v_all = a.vocab;
-  if (r >= min(*a.m_dev, a.m_upper)) return;
-  const int row = a.row_map ? a.row_map[r] : r;
-  const bool there = row >= 0 && row < a.n_rows;
-  const T* z = (const T*)a.logits + (size_t)(there ? row : 0) * a.row_stride;
-  const int share = (v_all + kThreads - 1) / kThreads, lo = min(tid * share, v_all), hi = there ? min(lo + share, v_all) : lo;
+// A row in pieces of 16 bytes a thread: piece c of thread t holds ids (c NT + t) kVec ..; what is past the row is -infinity.
+template <typename T, int NT>
+struct Row {
+  static constexpr int kVec = st<T>::kVec, kSpan = NT * kVec, kThreads = NT;
+  const T* z;
+  int vocab, wide;
 
-  // the first of the order, and how many may be drawn
-  uint64_t best = 0;                                      // key, then lowest id
-  int count = 0;
-  for (int i = lo; i < hi; ++i) {
-    const float x = st<T>::ld(z + i);
-    if (!allowed(x)) continue;
-    ++count;
-    best = max(best, (uint64_t)key_of(x) << 32 | (uint32_t)~i);
+  __device__ __forceinline__ int n() const { return (vocab + kSpan - 1) / kSpan; }
+  __device__ __forceinline__ uint4 fetch(int c) const {
+    const int id = c * kSpan + threadIdx.x * kVec;
+    if (wide && id + kVec <= vocab) return *reinterpret_cast<const uint4*>(z + id);
+    uint32_t w[4];
+    if constexpr (kVec == 8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = id + 2 * i < vocab ? __builtin_bit_cast(unsigned short, z[id + 2 * i]) : 0xff80u;
+        const uint32_t hi = id + 2 * i + 1 < vocab ? __builtin_bit_cast(unsigned short, z[id + 2 * i + 1]) : 0xff80u;
+        w[i] = lo | hi << 16;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = id + i < vocab ? __float_as_uint((float)z[id + i]) : 0xff800000u;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
-  for (int o = 32; o; o >>= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, o, 64));
-  if ((tid & 63) == 0) sh.sums[tid >> 6] = best;
+  __device__ __forceinline__ static float number(const uint4& p, int e) {
+    if constexpr (kVec == 8) {
+      const uint32_t w = e < 2 ? p.x : e < 4 ? p.y : e < 6 ? p.z : p.w;
+      return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    } else {
+      return __uint_as_float(e == 0 ? p.x : e == 1 ? p.y : e == 2 ? p.z : p.w);
+    }
+  }
+  // f(piece's number, its 16 bytes, first id): four pieces are worked on while the next four are on their way
+  template <typename F>
+  __device__ __forceinline__ void pieces(F f) const {
+    const int all = n();
+    uint4 next[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < all) next[i] = fetch(i);
+#pragma unroll 1
+    for (int c = 0; c < all; c += 4) {
+      uint4 now[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) now[i] = next[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + 4 + i < all) next[i] = fetch(c + 4 + i);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < all) {
+          f(c + i, now[i], (c + i) * kSpan + (int)threadIdx.x * kVec);
+          __builtin_amdgcn_sched_barrier(0);              // (one after another: registers)
+        }
+    }
+  }
+  // f(z)
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    pieces([&](int, const uint4& p, int) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f(number(p, e));
+    });
+  }
+};
+
+// The fewest of `there` equal weights that bring `above` to the goal
+__device__ inline uint64_t fewest(uint64_t above, uint64_t each, uint64_t there, double goal) {
+  uint64_t need = 1;
+  if (each > 0 && goal > (double)above) need = (uint64_t)fmax(1.0, fmin(floor((goal - (double)above) / (double)each), (double)there));
+  while (need > 1 && (double)(above + (need - 1) * each) >= goal) --need;
+  while (need < there && (double)(above + need * each) < goal) ++need;
+  return need < there ? need : there;
+}
+
+// The draw: weigh(piece, f) calls f(e, above, tie, weight) for each token of a piece: above the border, on it, and the weight of one above.  Of the
+// tokens on the border the first `need` weigh `each`.
+template <typename R, typename W>
+__device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs& a, int r, uint64_t need, uint64_t each, W weigh) {
+  constexpr int NT = R::kThreads, kParts = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), parts = row.n() * kParts;
+  uint32_t number = 0;                                    // of this wave, above the border
+  row.pieces([&](int c, const uint4& p, int) __attribute__((always_inline)) {
+    uint64_t sum = 0;
+    uint32_t ties = 0;
+    weigh(p, [&](int, bool above, bool tie, uint64_t w) __attribute__((always_inline)) {
+      sum += w;
+      number += __popcll(__ballot(above));
+      ties += __popcll(__ballot(tie));
+    });
+    sum = wave_scan(sum);
+    if (lane == 63) {
+      sh.part.sum[c * kParts + wave] = sum;
+      sh.part.ties[c * kParts + wave] = ties;
+    }
+  });
   __syncthreads();
-  for (int w = 0; w < kWaves; ++w) best = max(best, sh.sums[w]);
-  uint64_t whole;
-  if (tid == 0) sh.index = v_all;
-  before_me((uint64_t)count, sh, whole);
-  const int n = (int)whole;
+  // parts two neighbours a thread (half as many threads: fewer than 1024)
+  constexpr int kMine = kMaxParts / NT;
+  uint64_t ties[kMine], own[kMine], mine = 0, all, whole, above;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int at = tid * kMine + i;
+    ties[i] = at < parts ? sh.part.ties[at] : 0;
+    own[i] = at < parts ? sh.part.sum[at] : 0;
+    mine += ties[i];
+  }
+  uint64_t ties_at = before_me<NT>(mine, sh, all);
+  const uint64_t first_ties = ties_at;
+  mine = 0;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    own[i] += (ties_at < need ? min(ties[i], need - ties_at) : 0) * each;
+    ties_at += ties[i];
+    mine += own[i];
+  }
+  uint64_t before = before_me<NT>(mine, sh, whole);
+  const float u = a.uniform[r];
+  const double goal = (double)(u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f) * (double)whole;
+  ties_at = first_ties;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    if ((double)before <= goal && (double)(before + own[i]) > goal) {
+      sh.index = tid * kMine + i;
+      sh.found = before;
+      sh.found2 = ties_at;
+    }
+    before += own[i];
+    ties_at += ties[i];
+  }
+  if (a.kept) {
+    before_me<NT>(lane == 0 ? number : 0, sh, above);
+    if (tid == 0) a.kept[r] = (int32_t)(above + min(all, need));
+  }
+  __syncthreads();
+  if (sh.index % kParts != wave) return;
+  // the part that holds it, once more
+  const int c = sh.index / kParts, id = c * R::kSpan + tid * R::kVec;
+  const uint4 p = row.fetch(c);
+  uint64_t w[R::kVec];
+  uint32_t tie[R::kVec], my_ties = 0;
+  weigh(p, [&](int e, bool, bool is_tie, uint64_t v) __attribute__((always_inline)) {
+    w[e] = v;
+    my_ties += tie[e] = is_tie;
+  });
+  uint64_t at = sh.found2 + wave_scan(my_ties) - my_ties;
+  mine = 0;
+#pragma unroll
+  for (int e = 0; e < R::kVec; ++e) {
+    if (tie[e] && at < need) w[e] = each;
+    at += tie[e];
+    mine += w[e];
+  }
+  uint64_t run = sh.found + wave_scan(mine) - mine;
+#pragma unroll
+  for (int e = 0; e < R::kVec; ++e) {
+    if ((double)run <= goal && (double)(run + w[e]) > goal) {
+      a.token[r] = id + e;
+      if (a.prob) a.prob[r] = (float)((double)w[e] / (double)whole);
+    }
+    run += w[e];
+  }
+}
+
+// Bins of bf16 numbers: 0 is the largest; the tiny numbers of both signs share one; b is monotone in z.
+struct Bins {
+  int top, positive, shift, tiny;                         // positive: bins above the tiny ones; shift: ranks that share theirs, less one
+  int allowed, n;                                         // bins of all finite numbers and infinity; of these, counted ones
+  __device__ explicit Bins(int top_rank) : top(top_rank) {
+    positive = max(0, top - kTiny + 1);
+    const int tiny_end = max(0, top + kTiny);             // in ranks below the top
+    shift = max(0, tiny_end - positive - 1);
+    tiny = tiny_end > 0 ? positive : -1;
+    allowed = top + 0x7f80 - shift;
+    n = min(kBins, allowed);
+  }
+  __device__ int of(float z) const {
+    const int d = top - rank_of(z);
+    return max(min(d, positive), d - shift);
+  }
+  __device__ float number(int b) const { return of_rank(b < positive ? top - b : top - b - shift); }
+  // of two numbers; NaNs and -infinity come out as `allowed` or more
+  __device__ __forceinline__ u16x2 of_two(uint32_t w) const {
+    const u16x2 d = __builtin_bit_cast(u16x2, (s16x2{(short)top, (short)top}) - ranks_of(w));
+    const u16x2 p = {(unsigned short)positive, (unsigned short)positive}, s = {(unsigned short)shift, (unsigned short)shift};
+    return __builtin_elementwise_max(__builtin_elementwise_min(d, p), __builtin_elementwise_sub_sat(d, s));
+  }
+};
+
+// f(e, bin) for the eight numbers of a piece; bins from `most` on are `most`
+template <typename F>
+__device__ __forceinline__ void each_bin(const Bins& bins, int most, const uint4& piece, F f) {
+  const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+  const u16x2 limit = {(unsigned short)most, (unsigned short)most};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(bins.of_two(w[i]), limit));
+    f(2 * i, (int)(b & 0xffff));
+    f(2 * i + 1, (int)(b >> 16));
+  }
+}
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  Shared& sh = *reinterpret_cast<Shared*>(lds);
+  constexpr int kWaves = NT / 64;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (r >= min(*a.m_dev, a.m_upper)) return;
+  const int at = a.row_map ? a.row_map[r] : r;
+  const bool there = at >= 0 && at < a.n_rows;
+  Row<T, NT> row;
+  row.z = (const T*)a.logits + (size_t)(there ? at : 0) * a.row_stride;
+  row.vocab = there ? a.vocab : 0;
+  row.wide = a.wide;
   const float heat = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
   const int k = a.top_k ? a.top_k[r] : 0;
-  if (n == 0 || !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f) {      // one token at most
+  if (tid < 256) sh.powers[tid] = exp2(tid / 256.0);
+
+  float most = -__builtin_inff();
+  row.each([&](float z) __attribute__((always_inline)) { most = fmaxf(most, z); });
+  most = wave_max(most);
+  if (lane == 0) sh.most[wave] = most;
+  __syncthreads();
+  most = wave_max(lane < kWaves ? sh.most[lane] : -__builtin_inff());
+  if (!allowed(most)) {
     if (tid == 0) {
-      a.token[r] = n ? (int32_t)~(uint32_t)best : 0;
-      if (a.prob) a.prob[r] = n ? 1.f : 0.f;
-      if (a.kept) a.kept[r] = n ? 1 : 0;
+      a.token[r] = 0;
+      if (a.prob) a.prob[r] = 0.f;
+      if (a.kept) a.kept[r] = 0;
     }
     return;
   }
-  const float most = of_key((uint32_t)(best >> 32));
-  uint32_t last_key = 0;                                  // kept: allowed, and key above last_key, or the same and id <= last_id
-  int last_id = v_all;
-  auto is_kept = [&](float x, int i) {
-    const uint32_t key = key_of(x);
-    return allowed(x) && (key > last_key || (key == last_key && i <= last_id));
-  };
-  // Narrow what is kept to the fewest whose count (or weight) reaches the goal: the key byte by byte, then the id.
-  auto narrow = [&](bool by_weight, double goal) {
-    uint32_t prefix = 0;
-    uint64_t above = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kThreads) sh.bins[i] = 0;
+  const bool one = !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f;       // the first of the order alone
+  const bool by_count = k > 0 && k < a.vocab && !one, by_mass = p < 1.f && !one;
+  const double enough = least > 0.f && !one ? (double)least * kUnit : 0.0;
+  const Weigher weight{(double)most, 369.32993046757463 / (double)heat, sh.powers};
+
+  if constexpr (sizeof(T) == 2) {
+    const Bins bins(rank_of(most));
+    int border = bins.allowed;                            // kept: bins below the border, and of the border's tokens the first `need`
+    uint64_t need = 0, each = 0;
+    // whether the bins do: a finite maximum, and no weight beyond them
+    bool counted = !one && most < __builtin_inff() && bins.tiny < kBins - 1 && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
+    if (one) {
+      // the bins of the largest and of everything else
+      if (bins.tiny != 0) {
+        counted = true;
+        border = 0;
+        need = 1;
+        each = (uint64_t)kUnit;
+      }
+    }
+    if (counted && (by_count || by_mass)) {
+      for (int i = tid; i < (kBins + 4) / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
       __syncthreads();
-      for (int i = lo; i < hi; ++i) {
-        const float x = st<T>::ld(z + i);
-        const uint32_t key = key_of(x);
-        if (!is_kept(x, i) || (shift < 24 && key >> (shift + 8) != prefix)) continue;
-        atomicAdd((unsigned long long*)&sh.bins[key >> shift & 255], (unsigned long long)(by_weight ? weight_of(x, most, heat) : 1));
+      uint64_t tiny = 0;
+      row.pieces([&](int, const uint4& piece, int) __attribute__((always_inline)) {
+        each_bin(bins, kBins, piece, [&](int e, int b) __attribute__((always_inline)) {
+          atomicAdd(&sh.counts[b], 1u);
+          if (b == bins.tiny) tiny += weight(Row<T, NT>::number(piece, e));
+        });
+      });
+      before_me<NT>(tiny, sh, tiny);
+#pragma unroll
+      for (int i = 0; i < kGroups / kWaves; ++i) {
+        const int g = i * kWaves + wave, b = g * 64 + lane;
+        const uint32_t n = b < bins.n ? sh.counts[b] : 0;
+        uint64_t mass = 0, number = 0;
+        if (__ballot(n != 0)) {
+          mass = wave_scan(n == 0 ? 0 : b == bins.tiny ? tiny : n * weight(bins.number(b)));
+          number = wave_scan(n);
+        }
+        if (lane == 63) {
+          sh.group.mass[g] = mass;
+          sh.group.count[g] = (uint32_t)number;
+        }
       }
       __syncthreads();
-      if (tid == 0) {
-        int b = 255;
-        uint64_t sum = above;
-        while (b > 0 && (double)(sum + sh.bins[b]) < goal) sum += sh.bins[b--];
-        sh.found = sum;
-        sh.word = prefix << 8 | (uint32_t)b;
+      // every wave finds the borders on its own: two groups a lane
+      static_assert(kGroups <= 128, "two groups a lane");
+      uint64_t mass[2], count[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int g = 2 * lane + i;
+        mass[i] = g < kGroups ? sh.group.mass[g] : 0;
+        count[i] = g < kGroups ? sh.group.count[g] : 0;
+      }
+      const uint64_t mass_at = wave_scan(mass[0] + mass[1]), count_at = wave_scan(count[0] + count[1]), all = lane_of(count_at, 63);
+      uint64_t total = lane_of(mass_at, 63);
+#pragma unroll 1
+      for (int round = 0; round < 2; ++round) {
+        if (!(round ? by_mass : by_count)) continue;
+        if (!round && (uint64_t)k > all) {                // all tokens, if there are no more than those counted
+          counted = bins.n == bins.allowed;
+          if (!counted) break;
+          continue;
+        }
+        const double goal = round ? (double)p * (double)total : (double)k;
+        const int owner = __builtin_ctzll(__ballot((double)(round ? mass_at : count_at) >= goal || lane == 63));
+        const uint64_t m0 = lane_of(mass_at - mass[0] - mass[1], owner), c0 = lane_of(count_at - count[0] - count[1], owner);
+        const uint64_t m1 = m0 + lane_of(mass[0], owner), c1 = c0 + lane_of(count[0], owner);
+        const bool second = (double)(round ? m1 : c1) < goal;
+        const int b = (2 * owner + second) * 64 + lane;
+        const uint64_t n = b == border ? need : b < min(border, bins.n) ? sh.counts[b] : 0;
+        const uint64_t w = n && b != bins.tiny ? weight(bins.number(b)) : 0, here = n == 0 ? 0 : b == bins.tiny ? tiny : n * w;
+        const uint64_t masses = (second ? m1 : m0) + wave_scan(here), runs = round ? masses : (second ? c1 : c0) + wave_scan(n);
+        const int first = __builtin_ctzll(__ballot((double)runs >= goal || lane == 63));
+        const uint64_t n_there = lane_of(n, first), unit = round ? lane_of(w, first) : 1;
+        border = (2 * owner + second) * 64 + first;
+        if (border == bins.tiny) {
+          counted = false;
+          break;
+        }
+        need = fewest(lane_of(runs, first) - n_there * unit, unit, n_there, goal);
+        each = lane_of(w, first);
+        total = lane_of(masses - here, first) + need * each;
+      }
+    }
+    if (counted && enough > 0) {
+      // the first bin whose weight is not enough: near where the logarithm says
+      const int b = bins.of((float)((double)most + (double)heat * log((double)least))) - 31 + lane;
+      const bool tiny_first = (double)weight(of_rank(min(bins.top, kTiny - 1))) >= enough, tiny_last = (double)weight(of_rank(1 - kTiny)) >= enough;
+      const bool passes = b < 0 || (b < bins.n && (b == bins.tiny ? tiny_last : (double)weight(bins.number(b)) >= enough));
+      const uint64_t passing = __ballot(passes);
+      if (!(passing & 1) || passing >> 63 || (bins.tiny >= 0 && tiny_first != tiny_last)) {
+        counted = false;
+      } else {
+        const int limit = lane_of((uint64_t)(uint32_t)b, 0) + __builtin_ctzll(~passing);
+        if (limit <= border) {
+          border = limit;
+          need = 0;
+        }
+      }
+    }
+    if (counted) {
+      // weights of the bins that are kept, as far as they are not 0 (exp(-31.2) 2^44 is below 1/2), and a 0 for all others
+      const int table = max(0, min(min(border, bins.n), bins.of((float)((double)most - 31.2 * (double)heat)) + 2));
+      __syncthreads();
+      for (int b = tid; b <= table; b += NT) sh.weights[b] = b < table && b != bins.tiny ? weight(bins.number(b)) : 0;
+      __syncthreads();
+      const int tiny = bins.tiny < table ? bins.tiny : -1;
+      draw(row, sh, a, r, need, each, [&](const uint4& piece, auto f) __attribute__((always_inline)) {
+        each_bin(bins, bins.allowed, piece, [&](int e, int b) __attribute__((always_inline)) {
+          uint64_t w = sh.weights[min(b, table)];
+          if (b == tiny) w = weight(Row<T, NT>::number(piece, e));
+          f(e, b < border, b == border && need > 0, w);
+        });
+      });
+      return;
+    }
+  }
+
+  // the border's key digit by digit: by count, then by mass
+  uint32_t border = one ? key_of(most) : 0x007fffffu;     // (-infinity's)
+  uint64_t need = one, each = one ? (uint64_t)kUnit : 0;
+  auto inside = [&](uint32_t key, float z) __attribute__((always_inline)) { return allowed(z) && key >= border; };
+#pragma unroll 1
+  for (int round = 0; round < 2; ++round) {
+    if (!(round ? by_mass : by_count)) continue;
+    uint64_t total = 0;
+    row.each([&](float z) __attribute__((always_inline)) {
+      const uint32_t key = key_of(z);
+      if (allowed(z) && key > border) total += round ? weight(z) : 1;
+    });
+    before_me<NT>(total, sh, total);
+    if (!round && (uint64_t)k >= total) continue;
+    const double goal = round ? (double)p * (double)(total + need * each) : (double)k;
+    uint32_t prefix = 0;
+    uint64_t above = 0;
+    int shift = 32;
+#pragma unroll 1
+    for (int step = 0; step < 3; ++step) {
+      const int bits = step < 2 ? 11 : 10, upper = shift;
+      shift -= bits;
+      for (int i = tid; i < kDigits; i += NT) sh.digits[i] = 0;
+      __syncthreads();
+      row.each([&](float z) __attribute__((always_inline)) {
+        const uint32_t key = key_of(z);
+        if (inside(key, z) && (step == 0 || key >> upper == prefix))
+          atomicAdd((unsigned long long*)&sh.digits[key >> shift & ((1 << bits) - 1)], (unsigned long long)(round ? weight(z) : 1));
+      });
+      __syncthreads();
+      // neighbouring digits a thread, descending
+      constexpr int kMine = kDigits / NT;
+      const int top = (1 << bits) - 1 - kMine * tid;
+      uint64_t sum = 0, whole;
+      for (int i = 0; i < kMine; ++i) sum += top - i >= 0 ? sh.digits[top - i] : 0;
+      uint64_t run = above + before_me<NT>(sum, sh, whole);
+      if ((double)run < goal && (double)(run + sum) >= goal) {
+        int digit = top;
+        while ((double)(run + sh.digits[digit]) < goal) run += sh.digits[digit--];
+        sh.found = run;
+        sh.word = prefix << bits | (uint32_t)digit;
+        sh.found2 = sh.digits[digit];
       }
       __syncthreads();
       above = sh.found;
       prefix = sh.word;
     }
-    // of the tokens with that key, as many as it takes
-    const uint64_t each = by_weight ? weight_of(of_key(prefix), most, heat) : 1;
-    int ties = 0;
-    for (int i = lo; i < hi; ++i) {
-      const float x = st<T>::ld(z + i);
-      ties += is_kept(x, i) && key_of(x) == prefix;
-    }
-    uint64_t all_ties;
-    const uint64_t ties_before = before_me((uint64_t)ties, sh, all_ties);
-    uint64_t need = 1;
-    if (each > 0 && goal > (double)above) need = (uint64_t)max(1.0, floor((goal - (double)above) / (double)each));
-    while (need > 1 && (double)(above + (need - 1) * each) >= goal) --need;
-    while (need < all_ties && (double)(above + need * each) < goal) ++need;
-    if (need > all_ties) need = all_ties;
-    if (ties_before < need && need <= ties_before + ties) {
-      uint64_t seen = ties_before;
-      for (int i = lo; i < hi; ++i) {
-        const float x = st<T>::ld(z + i);
-        if (is_kept(x, i) && key_of(x) == prefix && ++seen == need) {
-          sh.index = i;
-          break;
-        }
-      }
-    }
+    // (tokens with the border's key of the first round: `need` of them, whatever the digits have added up)
+    const uint64_t w = weight(of_key(prefix)), unit = round ? w : 1;
+    need = fewest(above, unit, prefix == border ? need : unit ? sh.found2 / unit : 1, goal);
+    each = w;
+    border = prefix;
     __syncthreads();
-    last_id = sh.index;
-    last_key = prefix;
-    __syncthreads();
-  };
-  if (k > 0 && k < n) narrow(false, (double)k);
-  if (p < 1.f) {
-    uint64_t mine = 0;
-    for (int i = lo; i < hi; ++i) {
-      const float x = st<T>::ld(z + i);
-      if (is_kept(x, i)) mine += weight_of(x, most, heat);
-    }
-    before_me(mine, sh, whole);
-    narrow(true, (double)p * (double)whole);
   }
-  const double enough = least > 0.f ? (double)least * kUnit : 0.0;
-  uint64_t mine = 0, number = 0;
-  for (int i = lo; i < hi; ++i) {
-    const float x = st<T>::ld(z + i);
-    if (!is_kept(x, i)) continue;
-    const uint64_t w = weight_of(x, most, heat);
-    if (least > 0.f && (double)w < enough) continue;
-    mine += w;
-    ++number;
-  }
-  uint64_t numbers;
-  before_me(number, sh, numbers);
-  const uint64_t at = before_me(mine, sh, whole);
-  const float u = a.uniform[r];
-  const double goal = (double)(u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f) * (double)whole;
-  if ((double)at <= goal && (double)(at + mine) > goal) {
-    uint64_t sum = at;
-    for (int i = lo; i < hi; ++i) {
-      const float x = st<T>::ld(z + i);
-      if (!is_kept(x, i)) continue;
-      const uint64_t w = weight_of(x, most, heat);
-      if (least > 0.f && (double)w < enough) continue;
-      sum += w;
-      if ((double)sum > goal) {
-        a.token[r] = i;
-        if (a.prob) a.prob[r] = (float)((double)w / (double)whole);
-        if (a.kept) a.kept[r] = (int32_t)numbers;
-        break;
+  if (enough > 0 && (double)each < enough) need = 0;
+  draw(row, sh, a, r, need, each, [&](const uint4& piece, auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < Row<T, NT>::kVec; ++e) {
+      const float z = Row<T, NT>::number(piece, e);
+      const uint32_t key = key_of(z);
+      bool above = allowed(z) && key > border;
+      uint64_t w = 0;
+      if (above) {
+        w = weight(z);
+        above = (double)w >= enough;
       }
+      f(e, above, allowed(z) && key == border, above ? w : 0);
     }
-  }
+  });
 }
 
 }  // namespace
@@ -211,9 +560,21 @@ size_t slk_sample_filtered_bytes(int m_upper, int vocab) { return 256; }
 int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t row_stride, int n_rows, int vocab, const int32_t* row_map,
                         const int32_t* m_dev, int m_upper, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                         const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace) {
-  const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
-  if (dtype == SL_BF16) hipLaunchKernelGGL((sample_filtered_kernel<bf16_t>), dim3(m_upper), dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((sample_filtered_kernel<float>), dim3(m_upper), dim3(kThreads), 0, s, a);
+  const int wide = (uintptr_t)logits % 16 == 0 && row_stride * (int64_t)sl_tsize(dtype) % 16 == 0;
+  const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, wide, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
+#define SAMPLE_RUN(T, NT)                                                                                                  \
+  do {                                                                                                                     \
+    static unsigned long long done = 0;                                                                                    \
+    SL_ALLOW_DYNAMIC_LDS(done, (sample_filtered_kernel<T, NT>), sizeof(Shared));                                             \
+    hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), sizeof(Shared), s, a);                      \
+  } while (0)
+  const bool many = m_upper > 256;
+  if (dtype == SL_BF16) {
+    if (many) SAMPLE_RUN(bf16_t, 512); else SAMPLE_RUN(bf16_t, 1024);
+  } else {
+    if (many) SAMPLE_RUN(float, 512); else SAMPLE_RUN(float, 1024);
+  }
+#undef SAMPLE_RUN
   SL_LAUNCH_CHECK();
   return SL_OK;
 }
