@@ -4,12 +4,12 @@
 // and, in order of ids, some of those that equal it.  Weights are whole numbers, W = rint(2^44 exp((z - max) / T)): at most 2^18 of them
 // add up to less than 2^63, in any order and from any thread, to the same sum.
 //
-// A workgroup takes a row and passes over it as often as it has to, 64 bytes a thread in flight.
+// A workgroup takes a row and passes over it as often as it has to, 32 to 64 bytes a thread in flight.
 //
 // Weights.  2^t = 2^n T[i] 2^(r / 256) with 256 t = 256 n + i + r, |r| <= 1 / 2: a table of 256 powers and a sum of four terms, off by
 // less than 2^-51 of itself.
 // bf16.  A weight depends on 16 bits, and logits take a few thousand of the 65536 numbers.  These are counted one by one (LDS, an atomic
-// add of one a token): order, sums of weights and borders follow from counts times weights, 64 numbers a wave and step, and the exponential is
+// add of one a token): order, sums of weights and borders follow from counts times weights, and the exponential is
 // taken once for each number that occurs; the last pass reads the weights of what is kept from a table.  Numbers below 2^-10 in size, nearly
 // half of the 65536 and hardly any logit, share one bin and are weighed token by token.
 // fp32, and bf16 where that does not do (a border among the tiny numbers, a temperature in the hundreds): the border's key in three
@@ -18,7 +18,7 @@
 
 namespace {
 
-constexpr int kBins = 6144, kGroups = kBins / 64, kDigits = 2048;
+constexpr int kBins = 6144, kDigits = 2048;
 constexpr int kTiny = 0x3a80;                             // rank of 2^-10
 constexpr int kMaxParts = 1024;                           // 64 times 16 bytes of 1024 threads: 2^18 fp32 numbers
 constexpr double kUnit = 17592186044416.0;                // 2^44
@@ -26,7 +26,7 @@ constexpr double kUnit = 17592186044416.0;                // 2^44
 struct SampleArgs {
   const void* logits;
   int64_t row_stride;
-  int n_rows, vocab, m_upper, wide;                       // wide: every row is 16-byte aligned
+  int n_rows, vocab, m_upper;
   const int32_t *row_map, *m_dev, *top_k;
   const float *temperature, *top_p, *min_p, *uniform;
   int32_t* token;
@@ -40,24 +40,19 @@ struct Shared {
     uint64_t weights[kBins + 4];
     uint64_t digits[kDigits];
   };
-  union {
-    struct {
-      uint64_t mass[kGroups];
-      uint32_t count[kGroups];
-    } group;
-    struct {                                              // of a wave's part of a piece, in order of ids
-      uint64_t sum[kMaxParts];
-      uint32_t ties[kMaxParts];
-    } part;
-  };
+  struct {                                                // of a wave's part of a piece, in order of ids
+    uint64_t sum[kMaxParts];
+    uint32_t ties[kMaxParts];
+  } part;
   double powers[256];
   uint64_t sums[16], sums2[16];
+  uint32_t numbers[16];
   uint64_t found, found2;
   uint32_t word;
   int index;
   float most[16];
 };
-static_assert(sizeof(Shared) <= 80 * 1024, "two workgroups a CU");
+static_assert(sizeof(Shared) <= 64 * 1024, "two workgroups a CU");
 
 // fp32 as a number whose order is that of z (both zeros alike)
 __device__ inline uint32_t key_of(float z) {
@@ -68,13 +63,9 @@ __device__ inline float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31
 // a token that may be drawn: neither NaN nor -infinity
 __device__ inline bool allowed(float z) { return z > -__builtin_inff(); }
 
-// Two bf16 numbers as 16-bit integers whose order is that of the numbers, both zeros alike; above +infinity's and below -infinity's are NaNs.
+// A bf16 number's rank: a 16-bit integer whose order is that of the numbers, both zeros alike; above +infinity's and below -infinity's are NaNs.
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-__device__ inline s16x2 ranks_of(uint32_t w) {
-  const s16x2 x = __builtin_bit_cast(s16x2, w), sign = x >> 15;
-  return (x ^ (sign & (short)0x7fff)) - sign;
-}
 __device__ inline int rank_of(float z) {
   const uint32_t bits = __float_as_uint(z) >> 16;
   return bits >> 15 ? -(int)(bits & 0x7fff) : (int)bits;
@@ -84,7 +75,7 @@ __device__ inline float of_rank(int r) { return __uint_as_float((uint32_t)(r < 0
 struct Weigher {
   double most, rate;                                      // rate: 256 log2(e) / temperature
   const double* powers;
-  __device__ uint64_t operator()(float z) const {
+  __device__ __forceinline__ uint64_t operator()(float z) const {
     constexpr double kRound = 6755399441055744.0, L = 0.0027076061740622863;      // 1.5 2^52; ln 2 / 256
     if ((double)z == most) return (uint64_t)kUnit;        // (an infinity, too)
     const double t = fmax(((double)z - most) * rate, -16384.0), y = t + kRound, r = (t - (y - kRound)) * L;
@@ -110,10 +101,18 @@ __device__ inline uint64_t wave_scan(uint64_t v) {
   v += moved<0x143, 12>(v);                               // lane 31 to the upper half
   return v;
 }
+__device__ inline uint32_t wave_scan32(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 10, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 12, 15, true);
+  return v;
+}
 __device__ inline uint64_t lane_of(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
 }
-__device__ inline uint64_t wave_total(uint64_t v) { return lane_of(wave_scan(v), 63); }
 
 // sum over the block of the threads before this one; `whole` gets the sum of all
 template <int NT>
@@ -128,68 +127,96 @@ __device__ inline uint64_t before_me(uint64_t v, Shared& sh, uint64_t& whole) {
   return (wave ? lane_of(waves, wave - 1) : 0) + sum - v;
 }
 
-// A row in pieces of 16 bytes a thread: piece c of thread t holds ids (c NT + t) kVec ..; what is past the row is -infinity.
+// two sums at once, in place
+template <int NT>
+__device__ inline void before_me2(uint64_t& v, uint32_t& n, Shared& sh, uint64_t& v_all, uint32_t& n_all) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t sum = wave_scan(v);
+  const uint32_t number = wave_scan32(n);
+  __syncthreads();
+  if (lane == 63) {
+    sh.sums[wave] = sum;
+    sh.sums2[wave] = number;
+  }
+  __syncthreads();
+  const uint64_t waves = wave_scan(lane < NT / 64 ? sh.sums[lane] : 0), numbers = wave_scan(lane < NT / 64 ? sh.sums2[lane] : 0);
+  v_all = lane_of(waves, NT / 64 - 1);
+  n_all = (uint32_t)lane_of(numbers, NT / 64 - 1);
+  v = (wave ? lane_of(waves, wave - 1) : 0) + sum - v;
+  n = (uint32_t)(wave ? lane_of(numbers, wave - 1) : 0) + number - n;
+}
+
+typedef uint32_t piece_t __attribute__((ext_vector_type(4), aligned(2)));
+
+// A row in pieces of 16 bytes a thread: piece c of thread t holds ids (c NT + t) kVec ..; what is past the row is -infinity.  Rows begin where
+// they like (the loads take any address).
 template <typename T, int NT>
 struct Row {
-  static constexpr int kVec = st<T>::kVec, kSpan = NT * kVec, kThreads = NT;
+  static constexpr int kVec = st<T>::kVec, kSpan = NT * kVec, kThreads = NT, kBits = 128 / kVec;
   const T* z;
-  int vocab, wide;
+  int vocab;
 
   __device__ __forceinline__ int n() const { return (vocab + kSpan - 1) / kSpan; }
   __device__ __forceinline__ uint4 fetch(int c) const {
-    const int id = c * kSpan + threadIdx.x * kVec;
-    if (wide && id + kVec <= vocab) return *reinterpret_cast<const uint4*>(z + id);
-    uint32_t w[4];
-    if constexpr (kVec == 8) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = id + 2 * i < vocab ? __builtin_bit_cast(unsigned short, z[id + 2 * i]) : 0xff80u;
-        const uint32_t hi = id + 2 * i + 1 < vocab ? __builtin_bit_cast(unsigned short, z[id + 2 * i + 1]) : 0xff80u;
-        w[i] = lo | hi << 16;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = id + i < vocab ? __float_as_uint((float)z[id + i]) : 0xff800000u;
+    const int id = c * kSpan + threadIdx.x * kVec, over = id + kVec - vocab;
+    if (over <= 0) {
+      const piece_t p = *reinterpret_cast<const piece_t*>(z + id);
+      return make_uint4(p.x, p.y, p.z, p.w);
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    // the row's end: its last 16 bytes, moved down, and -infinities
+    constexpr uint64_t kNone = kVec == 8 ? 0xff80ff80ff80ff80ull : 0xff800000ff800000ull;
+    uint64_t lo = kNone, hi = kNone;
+    if (over < kVec) {
+      if (vocab >= kVec) {
+        const piece_t p = *reinterpret_cast<const piece_t*>(z + vocab - kVec);
+        lo = (uint64_t)p.y << 32 | p.x;
+        hi = (uint64_t)p.w << 32 | p.z;
+#pragma unroll 1
+        for (int i = 0; i < over; ++i) {
+          lo = lo >> kBits | hi << (64 - kBits);
+          hi = hi >> kBits | kNone << (64 - kBits);
+        }
+      } else {                                            // (a row of less than 16 bytes)
+#pragma unroll 1
+        for (int i = vocab - 1; i >= 0; --i) {
+          hi = hi << kBits | lo >> (64 - kBits);
+          if constexpr (kVec == 8) lo = lo << kBits | __builtin_bit_cast(unsigned short, z[i]);
+          else lo = lo << kBits | __float_as_uint((float)z[i]);
+        }
+      }
+    }
+    return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
   }
   __device__ __forceinline__ static float number(const uint4& p, int e) {
+    const uint32_t x = p.x, y = p.y, z = p.z, w = p.w;    // (values: of references the compiler makes a place in memory)
     if constexpr (kVec == 8) {
-      const uint32_t w = e < 2 ? p.x : e < 4 ? p.y : e < 6 ? p.z : p.w;
-      return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+      const uint32_t u = e < 4 ? e < 2 ? x : y : e < 6 ? z : w;
+      return __uint_as_float(e & 1 ? u & 0xffff0000u : u << 16);
     } else {
-      return __uint_as_float(e == 0 ? p.x : e == 1 ? p.y : e == 2 ? p.z : p.w);
+      return __uint_as_float(e < 2 ? e == 0 ? x : y : e == 2 ? z : w);
     }
   }
-  // f(piece's number, its 16 bytes, first id): four pieces are worked on while the next four are on their way
+  // f(piece's number, its 16 bytes): two pieces are worked on while the next two are on their way
   template <typename F>
   __device__ __forceinline__ void pieces(F f) const {
     const int all = n();
-    uint4 next[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < all) next[i] = fetch(i);
+    uint4 a = all > 0 ? fetch(0) : make_uint4(0, 0, 0, 0), b = all > 1 ? fetch(1) : a;
 #pragma unroll 1
-    for (int c = 0; c < all; c += 4) {
-      uint4 now[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) now[i] = next[i];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + 4 + i < all) next[i] = fetch(c + 4 + i);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < all) {
-          f(c + i, now[i], (c + i) * kSpan + (int)threadIdx.x * kVec);
-          __builtin_amdgcn_sched_barrier(0);              // (one after another: registers)
-        }
+    for (int c = 0; c < all; c += 2) {
+      const uint4 p = a, q = b;
+      if (c + 2 < all) a = fetch(c + 2);
+      if (c + 3 < all) b = fetch(c + 3);
+      f(c, p);
+      __builtin_amdgcn_sched_barrier(0);                  // (one after another: registers)
+      if (c + 1 < all) f(c + 1, q);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // f(z)
-  template <typename F>
+  template <int UNROLL, typename F>
   __device__ __forceinline__ void each(F f) const {
-    pieces([&](int, const uint4& p, int) __attribute__((always_inline)) {
-#pragma unroll
+    pieces([&](int, const uint4& p) __attribute__((always_inline)) {
+#pragma unroll UNROLL
       for (int e = 0; e < kVec; ++e) f(number(p, e));
     });
   }
@@ -204,85 +231,94 @@ __device__ inline uint64_t fewest(uint64_t above, uint64_t each, uint64_t there,
   return need < there ? need : there;
 }
 
-// The draw: weigh(piece, f) calls f(e, above, tie, weight) for each token of a piece: above the border, on it, and the weight of one above.  Of the
-// tokens on the border the first `need` weigh `each`.
-template <typename R, typename W>
-__device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs& a, int r, uint64_t need, uint64_t each, W weigh) {
-  constexpr int NT = R::kThreads, kParts = NT / 64;
+// The draw: weigh(piece, f, g) calls f(e, tie, weight) for each token of a piece: whether it is on the border, and the weight of one above, and
+// g(e, weight) for what weighs more than f was told.  Of the tokens on the border the first `need` weigh `each`.  kept: the number of
+// tokens kept, or -1; then above(piece) counts a lane's tokens above the border.
+template <typename R, typename W, typename N>
+__device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs& a, int r, uint32_t need, uint64_t each, int kept, W weigh, N above) {
+  constexpr int NT = R::kThreads, kParts = NT / 64, kMine = kMaxParts / NT;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), parts = row.n() * kParts;
-  uint32_t number = 0;                                    // of this wave, above the border
-  row.pieces([&](int c, const uint4& p, int) __attribute__((always_inline)) {
+  const bool count = a.kept && kept < 0;
+  uint32_t number = 0;
+  row.pieces([&](int c, const uint4& p) __attribute__((always_inline)) {
     uint64_t sum = 0;
     uint32_t ties = 0;
-    weigh(p, [&](int, bool above, bool tie, uint64_t w) __attribute__((always_inline)) {
+    weigh(p, [&](int, bool tie, uint64_t w) __attribute__((always_inline)) {
       sum += w;
-      number += __popcll(__ballot(above));
       ties += __popcll(__ballot(tie));
-    });
+    }, [&](int, uint64_t w) __attribute__((always_inline)) { sum += w; });
+    if (count) number += above(p);
     sum = wave_scan(sum);
     if (lane == 63) {
       sh.part.sum[c * kParts + wave] = sum;
       sh.part.ties[c * kParts + wave] = ties;
     }
   });
+  if (count) number = wave_scan32(number);
+  if (lane == 63) sh.numbers[wave] = number;
   __syncthreads();
-  // parts two neighbours a thread (half as many threads: fewer than 1024)
-  constexpr int kMine = kMaxParts / NT;
-  uint64_t ties[kMine], own[kMine], mine = 0, all, whole, above;
+  // sums up to each part, neighbouring parts a thread
+  uint64_t sums = 0;
+  uint32_t ties = 0;
 #pragma unroll
   for (int i = 0; i < kMine; ++i) {
     const int at = tid * kMine + i;
-    ties[i] = at < parts ? sh.part.ties[at] : 0;
-    own[i] = at < parts ? sh.part.sum[at] : 0;
-    mine += ties[i];
+    if (at < parts) {
+      sums += sh.part.sum[at];
+      ties += sh.part.ties[at];
+    }
   }
-  uint64_t ties_at = before_me<NT>(mine, sh, all);
-  const uint64_t first_ties = ties_at;
-  mine = 0;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    own[i] += (ties_at < need ? min(ties[i], need - ties_at) : 0) * each;
-    ties_at += ties[i];
-    mine += own[i];
-  }
-  uint64_t before = before_me<NT>(mine, sh, whole);
+  uint64_t all_sums;
+  uint32_t all_ties;
+  const uint64_t own_sums = sums;
+  const uint32_t own_ties = ties;
+  before_me2<NT>(sums, ties, sh, all_sums, all_ties);
+  const uint64_t whole = all_sums + min(all_ties, need) * each;
   const float u = a.uniform[r];
   const double goal = (double)(u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f) * (double)whole;
-  ties_at = first_ties;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    if ((double)before <= goal && (double)(before + own[i]) > goal) {
-      sh.index = tid * kMine + i;
-      sh.found = before;
-      sh.found2 = ties_at;
+  if ((double)(sums + min(ties, need) * each) <= goal && (double)(sums + own_sums + min(ties + own_ties, need) * each) > goal) {
+    int at = tid * kMine;
+    for (; at < tid * kMine + kMine - 1; ++at) {
+      const uint64_t s = sums + sh.part.sum[at];
+      const uint32_t t = ties + sh.part.ties[at];
+      if ((double)(s + min(t, need) * each) > goal) break;
+      sums = s;
+      ties = t;
     }
-    before += own[i];
-    ties_at += ties[i];
+    sh.index = at;
+    sh.found = sums;
+    sh.word = ties;
   }
-  if (a.kept) {
-    before_me<NT>(lane == 0 ? number : 0, sh, above);
-    if (tid == 0) a.kept[r] = (int32_t)(above + min(all, need));
+  if (a.kept && tid == 0) {
+    if (count) {
+      kept = (int)min(all_ties, need);
+      for (int w = 0; w < kParts; ++w) kept += (int)sh.numbers[w];
+    }
+    a.kept[r] = kept;
   }
   __syncthreads();
   if (sh.index % kParts != wave) return;
   // the part that holds it, once more
   const int c = sh.index / kParts, id = c * R::kSpan + tid * R::kVec;
   const uint4 p = row.fetch(c);
-  uint64_t w[R::kVec];
+  uint64_t w[R::kVec], mine = 0;
   uint32_t tie[R::kVec], my_ties = 0;
-  weigh(p, [&](int e, bool, bool is_tie, uint64_t v) __attribute__((always_inline)) {
+  weigh(p, [&](int e, bool is_tie, uint64_t v) __attribute__((always_inline)) {
     w[e] = v;
     my_ties += tie[e] = is_tie;
+  }, [&](int e, uint64_t v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < R::kVec; ++i) w[i] += i == e ? v : 0;
   });
-  uint64_t at = sh.found2 + wave_scan(my_ties) - my_ties;
-  mine = 0;
+  uint32_t at = sh.word + wave_scan32(my_ties) - my_ties;
+  const uint32_t taken = min(sh.word, need);
 #pragma unroll
   for (int e = 0; e < R::kVec; ++e) {
     if (tie[e] && at < need) w[e] = each;
     at += tie[e];
     mine += w[e];
   }
-  uint64_t run = sh.found + wave_scan(mine) - mine;
+  uint64_t run = sh.found + taken * each + wave_scan(mine) - mine;
 #pragma unroll
   for (int e = 0; e < R::kVec; ++e) {
     if ((double)run <= goal && (double)(run + w[e]) > goal) {
@@ -310,31 +346,64 @@ struct Bins {
     return max(min(d, positive), d - shift);
   }
   __device__ float number(int b) const { return of_rank(b < positive ? top - b : top - b - shift); }
-  // of two numbers; NaNs and -infinity come out as `allowed` or more
-  __device__ __forceinline__ u16x2 of_two(uint32_t w) const {
-    const u16x2 d = __builtin_bit_cast(u16x2, (s16x2{(short)top, (short)top}) - ranks_of(w));
+  // of two numbers in each word; NaNs and -infinity come out as `allowed` or more.  (Step by step for all four: each step waits for the one before.)
+  __device__ __forceinline__ void of_eight(const uint32_t (&w)[4], u16x2 (&out)[4]) const {
     const u16x2 p = {(unsigned short)positive, (unsigned short)positive}, s = {(unsigned short)shift, (unsigned short)shift};
-    return __builtin_elementwise_max(__builtin_elementwise_min(d, p), __builtin_elementwise_sub_sat(d, s));
+    const s16x2 t = {(short)top, (short)top};
+    s16x2 sign[4], rank[4];
+    u16x2 low[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sign[i] = __builtin_bit_cast(s16x2, w[i]) >> 15;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rank[i] = __builtin_bit_cast(s16x2, w[i]) ^ (sign[i] & (short)0x7fff);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rank[i] = sign[i] - rank[i];         // (less the rank: both zeros alike)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(u16x2, t + rank[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) low[i] = __builtin_elementwise_min(out[i], p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = __builtin_elementwise_sub_sat(out[i], s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = __builtin_elementwise_max(low[i], out[i]);
   }
 };
 
-// f(e, bin) for the eight numbers of a piece; bins from `most` on are `most`
-template <typename F>
-__device__ __forceinline__ void each_bin(const Bins& bins, int most, const uint4& piece, F f) {
+// f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on are `most`.  Returns whether one of them is tiny.
+template <int SIZE, typename F>
+__device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4& piece, F f) {
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
-  const u16x2 limit = {(unsigned short)most, (unsigned short)most};
+  const u16x2 limit = {(unsigned short)most, (unsigned short)most}, tiny = {(unsigned short)bins.tiny, (unsigned short)bins.tiny};
+  u16x2 two[4], other = {0xffff, 0xffff};
+  bins.of_eight(w, two);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) two[i] = __builtin_elementwise_min(two[i], limit);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(bins.of_two(w[i]), limit));
-    f(2 * i, (int)(b & 0xffff));
-    f(2 * i + 1, (int)(b >> 16));
+    other = __builtin_elementwise_min(other, two[i] ^ tiny);
+    const uint32_t b = __builtin_bit_cast(uint32_t, two[i] * (unsigned short)SIZE);
+    f(2 * i, b & 0xffff);
+    f(2 * i + 1, b >> 16);
+  }
+  return other[0] == 0 || other[1] == 0;
+}
+
+// f(e) for the tiny numbers of a piece
+template <typename F>
+__device__ __forceinline__ void each_tiny(const uint4& piece, F f) {
+  const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
+  uint32_t mask = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) mask |= ((w[e / 2] >> (e & 1 ? 16 : 0)) & 0x7fff) < (uint32_t)kTiny ? 1u << e : 0;
+  while (mask) {
+    f(__builtin_ctz(mask));
+    mask &= mask - 1;
   }
 }
 
 template <typename T, int NT>
 __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  Shared& sh = *reinterpret_cast<Shared*>(lds);
+  __shared__ __attribute__((aligned(16))) Shared sh;
   constexpr int kWaves = NT / 64;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (r >= min(*a.m_dev, a.m_upper)) return;
@@ -343,13 +412,12 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   Row<T, NT> row;
   row.z = (const T*)a.logits + (size_t)(there ? at : 0) * a.row_stride;
   row.vocab = there ? a.vocab : 0;
-  row.wide = a.wide;
   const float heat = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
   const int k = a.top_k ? a.top_k[r] : 0;
   if (tid < 256) sh.powers[tid] = exp2(tid / 256.0);
 
   float most = -__builtin_inff();
-  row.each([&](float z) __attribute__((always_inline)) { most = fmaxf(most, z); });
+  row.template each<8>([&](float z) __attribute__((always_inline)) { most = fmaxf(most, z); });
   most = wave_max(most);
   if (lane == 0) sh.most[wave] = most;
   __syncthreads();
@@ -370,7 +438,9 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   if constexpr (sizeof(T) == 2) {
     const Bins bins(rank_of(most));
     int border = bins.allowed;                            // kept: bins below the border, and of the border's tokens the first `need`
-    uint64_t need = 0, each = 0;
+    uint32_t need = 0;
+    uint64_t each = 0;
+    int kept = one ? 1 : -1;
     // whether the bins do: a finite maximum, and no weight beyond them
     bool counted = !one && most < __builtin_inff() && bins.tiny < kBins - 1 && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
     if (one) {
@@ -386,66 +456,62 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       for (int i = tid; i < (kBins + 4) / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
       __syncthreads();
       uint64_t tiny = 0;
-      row.pieces([&](int, const uint4& piece, int) __attribute__((always_inline)) {
-        each_bin(bins, kBins, piece, [&](int e, int b) __attribute__((always_inline)) {
-          atomicAdd(&sh.counts[b], 1u);
-          if (b == bins.tiny) tiny += weight(Row<T, NT>::number(piece, e));
+      row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
+        const bool small = each_bin<4>(bins, kBins, piece, [&](int, uint32_t at) __attribute__((always_inline)) {
+          atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(sh.counts) + at), 1u);
         });
+        if (small) each_tiny(piece, [&](int e) __attribute__((always_inline)) { tiny += weight(Row<T, NT>::number(piece, e)); });
       });
       before_me<NT>(tiny, sh, tiny);
+      // neighbouring bins a thread
+      constexpr int kMine = kBins / NT;
+      uint64_t mass = 0, total;
+      uint32_t count = 0, all;
 #pragma unroll
-      for (int i = 0; i < kGroups / kWaves; ++i) {
-        const int g = i * kWaves + wave, b = g * 64 + lane;
+      for (int i = 0; i < kMine; ++i) {
+        const int b = tid * kMine + i;
         const uint32_t n = b < bins.n ? sh.counts[b] : 0;
-        uint64_t mass = 0, number = 0;
-        if (__ballot(n != 0)) {
-          mass = wave_scan(n == 0 ? 0 : b == bins.tiny ? tiny : n * weight(bins.number(b)));
-          number = wave_scan(n);
-        }
-        if (lane == 63) {
-          sh.group.mass[g] = mass;
-          sh.group.count[g] = (uint32_t)number;
-        }
+        count += n;
+        if (n) mass += b == bins.tiny ? tiny : n * weight(bins.number(b));
       }
-      __syncthreads();
-      // every wave finds the borders on its own: two groups a lane
-      static_assert(kGroups <= 128, "two groups a lane");
-      uint64_t mass[2], count[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int g = 2 * lane + i;
-        mass[i] = g < kGroups ? sh.group.mass[g] : 0;
-        count[i] = g < kGroups ? sh.group.count[g] : 0;
-      }
-      const uint64_t mass_at = wave_scan(mass[0] + mass[1]), count_at = wave_scan(count[0] + count[1]), all = lane_of(count_at, 63);
-      uint64_t total = lane_of(mass_at, 63);
+      const uint64_t my_mass = mass;
+      const uint32_t my_count = count;
+      before_me2<NT>(mass, count, sh, total, all);
 #pragma unroll 1
       for (int round = 0; round < 2; ++round) {
         if (!(round ? by_mass : by_count)) continue;
-        if (!round && (uint64_t)k > all) {                // all tokens, if there are no more than those counted
+        if (!round && (uint32_t)k > all) {                // all tokens, if there are no more than those counted
           counted = bins.n == bins.allowed;
           if (!counted) break;
           continue;
         }
         const double goal = round ? (double)p * (double)total : (double)k;
-        const int owner = __builtin_ctzll(__ballot((double)(round ? mass_at : count_at) >= goal || lane == 63));
-        const uint64_t m0 = lane_of(mass_at - mass[0] - mass[1], owner), c0 = lane_of(count_at - count[0] - count[1], owner);
-        const uint64_t m1 = m0 + lane_of(mass[0], owner), c1 = c0 + lane_of(count[0], owner);
-        const bool second = (double)(round ? m1 : c1) < goal;
-        const int b = (2 * owner + second) * 64 + lane;
-        const uint64_t n = b == border ? need : b < min(border, bins.n) ? sh.counts[b] : 0;
+        const double before = round ? (double)mass : (double)count, up_to = round ? (double)(mass + my_mass) : (double)(count + my_count);
+        if (before < goal && goal <= up_to) {
+          sh.index = tid;
+          sh.found = mass;
+          sh.word = count;
+        }
+        __syncthreads();
+        // every wave finds the number on its own
+        const int b = sh.index * kMine + lane;
+        const uint32_t n = lane >= kMine ? 0 : b == border ? need : b < min(border, bins.n) ? sh.counts[b] : 0;
         const uint64_t w = n && b != bins.tiny ? weight(bins.number(b)) : 0, here = n == 0 ? 0 : b == bins.tiny ? tiny : n * w;
-        const uint64_t masses = (second ? m1 : m0) + wave_scan(here), runs = round ? masses : (second ? c1 : c0) + wave_scan(n);
-        const int first = __builtin_ctzll(__ballot((double)runs >= goal || lane == 63));
-        const uint64_t n_there = lane_of(n, first), unit = round ? lane_of(w, first) : 1;
-        border = (2 * owner + second) * 64 + first;
+        const uint64_t masses = sh.found + wave_scan(here);
+        const uint32_t counts = sh.word + wave_scan32(n);
+        const int first = __builtin_ctzll(__ballot((round ? (double)masses : (double)counts) >= goal || lane == kMine - 1));
+        const uint32_t n_there = __builtin_amdgcn_readlane(n, first), n_before = __builtin_amdgcn_readlane(counts - n, first);
+        const uint64_t m_before = lane_of(masses - here, first);
+        border = sh.index * kMine + first;
         if (border == bins.tiny) {
           counted = false;
           break;
         }
-        need = fewest(lane_of(runs, first) - n_there * unit, unit, n_there, goal);
         each = lane_of(w, first);
-        total = lane_of(masses - here, first) + need * each;
+        need = round ? fewest(m_before, each, n_there, goal) : k - n_before;
+        kept = n_before + need;
+        total = m_before + need * each;
+        __syncthreads();
       }
     }
     if (counted && enough > 0) {
@@ -461,28 +527,33 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
         if (limit <= border) {
           border = limit;
           need = 0;
+          kept = -1;
         }
       }
     }
     if (counted) {
-      // weights of the bins that are kept, as far as they are not 0 (exp(-31.2) 2^44 is below 1/2), and a 0 for all others
+      // weights of the bins that are kept, as far as they are not 0 (exp(-31.2) 2^44 is below 1/2); a 0 for the border and one for all others
       const int table = max(0, min(min(border, bins.n), bins.of((float)((double)most - 31.2 * (double)heat)) + 2));
       __syncthreads();
-      for (int b = tid; b <= table; b += NT) sh.weights[b] = b < table && b != bins.tiny ? weight(bins.number(b)) : 0;
+      for (int b = tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != bins.tiny ? weight(bins.number(b)) : 0;
       __syncthreads();
-      const int tiny = bins.tiny < table ? bins.tiny : -1;
-      draw(row, sh, a, r, need, each, [&](const uint4& piece, auto f) __attribute__((always_inline)) {
-        each_bin(bins, bins.allowed, piece, [&](int e, int b) __attribute__((always_inline)) {
-          uint64_t w = sh.weights[min(b, table)];
-          if (b == tiny) w = weight(Row<T, NT>::number(piece, e));
-          f(e, b < border, b == border && need > 0, w);
+      const uint32_t on_border = need > 0 && border == table ? border * 8 : 0xffff;      // (tokens of a border further down weigh nothing)
+      draw(row, sh, a, r, need, each, kept, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
+        const bool small = each_bin<8>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
+          f(e, at == on_border, *reinterpret_cast<const uint64_t*>(reinterpret_cast<const unsigned char*>(sh.weights) + at));
         });
+        if (small && bins.tiny < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
+      }, [&](const uint4& piece) __attribute__((always_inline)) {
+        uint32_t n = 0;
+        each_bin<1>(bins, bins.allowed, piece, [&](int, uint32_t b) __attribute__((always_inline)) { n += (int)b < border; });
+        return n;
       });
       return;
     }
   }
 
   // the border's key digit by digit: by count, then by mass
+  constexpr int kSlow = sizeof(T) == 2 ? 1 : 4;           // (of bf16 rows few come here)
   uint32_t border = one ? key_of(most) : 0x007fffffu;     // (-infinity's)
   uint64_t need = one, each = one ? (uint64_t)kUnit : 0;
   auto inside = [&](uint32_t key, float z) __attribute__((always_inline)) { return allowed(z) && key >= border; };
@@ -490,7 +561,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   for (int round = 0; round < 2; ++round) {
     if (!(round ? by_mass : by_count)) continue;
     uint64_t total = 0;
-    row.each([&](float z) __attribute__((always_inline)) {
+    row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
       const uint32_t key = key_of(z);
       if (allowed(z) && key > border) total += round ? weight(z) : 1;
     });
@@ -506,7 +577,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       shift -= bits;
       for (int i = tid; i < kDigits; i += NT) sh.digits[i] = 0;
       __syncthreads();
-      row.each([&](float z) __attribute__((always_inline)) {
+      row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
         const uint32_t key = key_of(z);
         if (inside(key, z) && (step == 0 || key >> upper == prefix))
           atomicAdd((unsigned long long*)&sh.digits[key >> shift & ((1 << bits) - 1)], (unsigned long long)(round ? weight(z) : 1));
@@ -536,20 +607,39 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     border = prefix;
     __syncthreads();
   }
-  if (enough > 0 && (double)each < enough) need = 0;
-  draw(row, sh, a, r, need, each, [&](const uint4& piece, auto f) __attribute__((always_inline)) {
+  if (enough > 0) {
+    uint32_t under = 0;                                   // the last key whose weight is not enough
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit; bit >>= 1)
+      if (under + bit < key_of(most) && (double)weight(of_key(under + bit)) < enough) under += bit;
+    if (under >= border) {
+      border = under;
+      need = 0;
+    }
+  }
+  draw(row, sh, a, r, need, each, one ? 1 : -1, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < Row<T, NT>::kVec; ++e) {
       const float z = Row<T, NT>::number(piece, e);
       const uint32_t key = key_of(z);
-      bool above = allowed(z) && key > border;
-      uint64_t w = 0;
-      if (above) {
-        w = weight(z);
-        above = (double)w >= enough;
-      }
-      f(e, above, allowed(z) && key == border, above ? w : 0);
+      const bool above = allowed(z) && key > border;
+      f(e, allowed(z) && key == border, sizeof(T) == 4 && above ? weight(z) : 0);
     }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const float z = Row<T, NT>::number(piece, e);
+        if (allowed(z) && key_of(z) > border) g(e, weight(z));
+      }
+    }
+  }, [&](const uint4& piece) __attribute__((always_inline)) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int e = 0; e < Row<T, NT>::kVec; ++e) {
+      const float z = Row<T, NT>::number(piece, e);
+      n += allowed(z) && key_of(z) > border;
+    }
+    return n;
   });
 }
 
@@ -560,14 +650,8 @@ size_t slk_sample_filtered_bytes(int m_upper, int vocab) { return 256; }
 int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t row_stride, int n_rows, int vocab, const int32_t* row_map,
                         const int32_t* m_dev, int m_upper, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                         const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace) {
-  const int wide = (uintptr_t)logits % 16 == 0 && row_stride * (int64_t)sl_tsize(dtype) % 16 == 0;
-  const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, wide, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
-#define SAMPLE_RUN(T, NT)                                                                                                  \
-  do {                                                                                                                     \
-    static unsigned long long done = 0;                                                                                    \
-    SL_ALLOW_DYNAMIC_LDS(done, (sample_filtered_kernel<T, NT>), sizeof(Shared));                                             \
-    hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), sizeof(Shared), s, a);                      \
-  } while (0)
+  const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
+#define SAMPLE_RUN(T, NT) hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), 0, s, a)
   const bool many = m_upper > 256;
   if (dtype == SL_BF16) {
     if (many) SAMPLE_RUN(bf16_t, 512); else SAMPLE_RUN(bf16_t, 1024);
