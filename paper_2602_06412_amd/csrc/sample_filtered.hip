@@ -36,8 +36,8 @@ struct SampleArgs {
 
 struct Shared {
   union {
-    uint32_t counts[kBins + 4];                           // (the last: what is beyond the bins)
-    uint64_t weights[kBins + 4];
+    uint32_t counts[kBins + 64];                          // (the last: what is beyond the bins, a place for each lane)
+    uint64_t weights[kBins + 2];
     uint64_t digits[kDigits];
   };
   struct {                                                // of a wave's part of a piece, in order of ids
@@ -47,7 +47,7 @@ struct Shared {
   double powers[256];
   uint64_t sums[16], sums2[16];
   uint32_t numbers[16];
-  uint64_t found, found2;
+  uint64_t found, found2, tiny;
   uint32_t word;
   int index;
   float most[16];
@@ -77,19 +77,20 @@ struct Weigher {
   const double* powers;
   __device__ __forceinline__ uint64_t operator()(float z) const {
     constexpr double kRound = 6755399441055744.0, L = 0.0027076061740622863;      // 1.5 2^52; ln 2 / 256
-    if ((double)z == most) return (uint64_t)kUnit;        // (an infinity, too)
     const double t = fmax(((double)z - most) * rate, -16384.0), y = t + kRound, r = (t - (y - kRound)) * L;
     const int n = (int)(uint32_t)__double_as_longlong(y);
     const double p = fma(r, fma(r, fma(r, fma(r, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0) * powers[n & 255];
-    return (uint64_t)__double_as_longlong(ldexp(p, 44 + (n >> 8)) + 4503599627370496.0) & 0xfffffffffffffull;
+    const uint64_t w = (uint64_t)__double_as_longlong(ldexp(p, 44 + (n >> 8)) + 4503599627370496.0) & 0xfffffffffffffull;
+    return (double)z == most ? (uint64_t)kUnit : w;       // (an infinity, too)
   }
 };
 
 // ---- sums over lanes, by moving lanes ----
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <int CTRL, int ROWS>
 __device__ inline uint64_t moved(uint64_t v) {
   const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 15, true), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 15, true);
-  return (uint64_t)hi << 32 | lo;
+  return __builtin_bit_cast(uint64_t, u32x2{lo, hi});
 }
 // of this lane and those before it
 __device__ inline uint64_t wave_scan(uint64_t v) {
@@ -225,7 +226,7 @@ struct Row {
 // The fewest of `there` equal weights that bring `above` to the goal
 __device__ inline uint64_t fewest(uint64_t above, uint64_t each, uint64_t there, double goal) {
   uint64_t need = 1;
-  if (each > 0 && goal > (double)above) need = (uint64_t)fmax(1.0, fmin(floor((goal - (double)above) / (double)each), (double)there));
+  if (each > 0 && goal > (double)above) need = (uint64_t)fmax(1.0, fmin(floor((goal - (double)above) * __builtin_amdgcn_rcp((double)each)), (double)there));      // (or one beside)
   while (need > 1 && (double)(above + (need - 1) * each) >= goal) --need;
   while (need < there && (double)(above + need * each) < goal) ++need;
   return need < there ? need : there;
@@ -301,8 +302,8 @@ __device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs&
   // the part that holds it, once more
   const int c = sh.index / kParts, id = c * R::kSpan + tid * R::kVec;
   const uint4 p = row.fetch(c);
-  uint64_t w[R::kVec], mine = 0;
-  uint32_t tie[R::kVec], my_ties = 0;
+  uint64_t w[R::kVec] = {}, mine = 0;
+  uint32_t tie[R::kVec] = {}, my_ties = 0;
   weigh(p, [&](int e, bool is_tie, uint64_t v) __attribute__((always_inline)) {
     w[e] = v;
     my_ties += tie[e] = is_tie;
@@ -370,7 +371,8 @@ struct Bins {
 };
 
 // f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on are `most`.  Returns whether one of them is tiny.
-template <int SIZE, typename F>
+// SKIP: f is not called if all numbers of the wave are from `most` on.
+template <int SIZE, bool SKIP = false, typename F>
 __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4& piece, F f) {
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
   const u16x2 limit = {(unsigned short)most, (unsigned short)most}, tiny = {(unsigned short)bins.tiny, (unsigned short)bins.tiny};
@@ -378,6 +380,10 @@ __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4
   bins.of_eight(w, two);
 #pragma unroll
   for (int i = 0; i < 4; ++i) two[i] = __builtin_elementwise_min(two[i], limit);
+  if (SKIP) {
+    const u16x2 first = __builtin_elementwise_min(__builtin_elementwise_min(two[0], two[1]), __builtin_elementwise_min(two[2], two[3]));
+    if (!__any(__builtin_bit_cast(uint32_t, first) != __builtin_bit_cast(uint32_t, limit))) return false;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     other = __builtin_elementwise_min(other, two[i] ^ tiny);
@@ -453,26 +459,35 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       }
     }
     if (counted && (by_count || by_mass)) {
-      for (int i = tid; i < (kBins + 4) / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
+      for (int i = tid; i < kBins / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
+      if (tid == 0) sh.tiny = 0;
       __syncthreads();
-      uint64_t tiny = 0;
       row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
-        const bool small = each_bin<4>(bins, kBins, piece, [&](int, uint32_t at) __attribute__((always_inline)) {
+        const bool small = each_bin<4>(bins, kBins + lane, piece, [&](int, uint32_t at) __attribute__((always_inline)) {
           atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(sh.counts) + at), 1u);
         });
-        if (small) each_tiny(piece, [&](int e) __attribute__((always_inline)) { tiny += weight(Row<T, NT>::number(piece, e)); });
+        if (small) each_tiny(piece, [&](int e) __attribute__((always_inline)) { atomicAdd((unsigned long long*)&sh.tiny, (unsigned long long)weight(Row<T, NT>::number(piece, e))); });
       });
-      before_me<NT>(tiny, sh, tiny);
+      __syncthreads();
       // neighbouring bins a thread
       constexpr int kMine = kBins / NT;
+      const uint64_t tiny = sh.tiny;
       uint64_t mass = 0, total;
-      uint32_t count = 0, all;
+      uint32_t n[kMine], count = 0, all;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int b = tid * kMine + i;
-        const uint32_t n = b < bins.n ? sh.counts[b] : 0;
-        count += n;
-        if (n) mass += b == bins.tiny ? tiny : n * weight(bins.number(b));
+        n[i] = sh.counts[b];
+        n[i] = b < bins.n ? n[i] : 0;
+        count += n[i];
+      }
+      if (__any(count > 0)) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+          const int b = tid * kMine + i;
+          const uint64_t w = n[i] * weight(bins.number(b));
+          mass += b == bins.tiny ? tiny : w;
+        }
       }
       const uint64_t my_mass = mass;
       const uint32_t my_count = count;
@@ -539,7 +554,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       __syncthreads();
       const uint32_t on_border = need > 0 && border == table ? border * 8 : 0xffff;      // (tokens of a border further down weigh nothing)
       draw(row, sh, a, r, need, each, kept, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
-        const bool small = each_bin<8>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
+        const bool small = each_bin<8, true>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
           f(e, at == on_border, *reinterpret_cast<const uint64_t*>(reinterpret_cast<const unsigned char*>(sh.weights) + at));
         });
         if (small && bins.tiny < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
