@@ -19,7 +19,8 @@
 namespace {
 
 constexpr int kBins = 6144, kDigits = 2048;
-constexpr int kTiny = 0x3a80;                             // rank of 2^-10
+constexpr int kTiny = 0x3a7f;                             // the largest bf16 below 2^-10: its 15 lower bits
+constexpr int kBelow = 1900;                              // bins that the largest number may be below 0: as far as -28
 constexpr int kMaxParts = 1024;                           // 64 times 16 bytes of 1024 threads: 2^18 fp32 numbers
 constexpr double kUnit = 17592186044416.0;                // 2^44
 
@@ -63,14 +64,8 @@ __device__ inline float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31
 // a token that may be drawn: neither NaN nor -infinity
 __device__ inline bool allowed(float z) { return z > -__builtin_inff(); }
 
-// A bf16 number's rank: a 16-bit integer whose order is that of the numbers, both zeros alike; above +infinity's and below -infinity's are NaNs.
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-__device__ inline int rank_of(float z) {
-  const uint32_t bits = __float_as_uint(z) >> 16;
-  return bits >> 15 ? -(int)(bits & 0x7fff) : (int)bits;
-}
-__device__ inline float of_rank(int r) { return __uint_as_float((uint32_t)(r < 0 ? 0x8000 - r : r) << 16); }
 
 struct Weigher {
   double most, rate;                                      // rate: 256 log2(e) / temperature
@@ -200,18 +195,34 @@ struct Row {
   // f(piece's number, its 16 bytes): two pieces are worked on while the next two are on their way
   template <typename F>
   __device__ __forceinline__ void pieces(F f) const {
-    const int all = n();
-    uint4 a = all > 0 ? fetch(0) : make_uint4(0, 0, 0, 0), b = all > 1 ? fetch(1) : a;
-#pragma unroll 1
-    for (int c = 0; c < all; c += 2) {
-      const uint4 p = a, q = b;
-      if (c + 2 < all) a = fetch(c + 2);
-      if (c + 3 < all) b = fetch(c + 3);
+    const int full = vocab / kSpan;
+    auto whole = [&](int c) __attribute__((always_inline)) {
+      const piece_t p = *reinterpret_cast<const piece_t*>(z + (size_t)c * kSpan + threadIdx.x * kVec);
+      return make_uint4(p.x, p.y, p.z, p.w);
+    };
+    auto work = [&](int c, const uint4& p) __attribute__((always_inline)) {
       f(c, p);
       __builtin_amdgcn_sched_barrier(0);                  // (one after another: registers)
-      if (c + 1 < all) f(c + 1, q);
-      __builtin_amdgcn_sched_barrier(0);
+    };
+    uint4 a[2] = {}, b[2] = {}, last = {};
+    if (full * kSpan < vocab) last = fetch(full);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (i < full) a[i] = whole(i);
+#pragma unroll 1
+    for (int c = 0; c < full; c += 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (c + 2 + i < full) b[i] = whole(c + 2 + i);
+      work(c, a[0]);
+      if (c + 1 < full) work(c + 1, a[1]);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (c + 4 + i < full) a[i] = whole(c + 4 + i);
+      if (c + 2 < full) work(c + 2, b[0]);
+      if (c + 3 < full) work(c + 3, b[1]);
     }
+    if (full * kSpan < vocab) work(full, last);
   }
   // f(z)
   template <int UNROLL, typename F>
@@ -330,68 +341,62 @@ __device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs&
   }
 }
 
-// Bins of bf16 numbers: 0 is the largest; the tiny numbers of both signs share one; b is monotone in z.
+// Bins of bf16 numbers, 0 the largest's, monotone in z.  With u = max(0, size - kTiny), sizes being the lower 15 bits, the bin is
+// middle - u for positive numbers and middle + u for negative ones: the tiny numbers of both signs are the middle bin, if that is a bin at all.
 struct Bins {
-  int top, positive, shift, tiny;                         // positive: bins above the tiny ones; shift: ranks that share theirs, less one
-  int allowed, n;                                         // bins of all finite numbers and infinity; of these, counted ones
-  __device__ explicit Bins(int top_rank) : top(top_rank) {
-    positive = max(0, top - kTiny + 1);
-    const int tiny_end = max(0, top + kTiny);             // in ranks below the top
-    shift = max(0, tiny_end - positive - 1);
-    tiny = tiny_end > 0 ? positive : -1;
-    allowed = top + 0x7f80 - shift;
+  int middle, allowed, n;                                 // bins of all numbers above -infinity; of these, counted ones
+  __device__ explicit Bins(float most) {
+    const int bits = (int)(__float_as_uint(most) >> 16), u = max(0, (bits & 0x7fff) - kTiny);
+    middle = bits >> 15 ? -u : u;
+    allowed = middle + 0x7f80 - kTiny;
     n = min(kBins, allowed);
   }
   __device__ int of(float z) const {
-    const int d = top - rank_of(z);
-    return max(min(d, positive), d - shift);
+    const int bits = (int)(__float_as_uint(z) >> 16), u = max(0, (bits & 0x7fff) - kTiny);
+    return bits >> 15 ? middle + u : middle - u;
   }
-  __device__ float number(int b) const { return of_rank(b < positive ? top - b : top - b - shift); }
-  // of two numbers in each word; NaNs and -infinity come out as `allowed` or more.  (Step by step for all four: each step waits for the one before.)
-  __device__ __forceinline__ void of_eight(const uint32_t (&w)[4], u16x2 (&out)[4]) const {
-    const u16x2 p = {(unsigned short)positive, (unsigned short)positive}, s = {(unsigned short)shift, (unsigned short)shift};
-    const s16x2 t = {(short)top, (short)top};
-    s16x2 sign[4], rank[4];
-    u16x2 low[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sign[i] = __builtin_bit_cast(s16x2, w[i]) >> 15;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rank[i] = __builtin_bit_cast(s16x2, w[i]) ^ (sign[i] & (short)0x7fff);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rank[i] = sign[i] - rank[i];         // (less the rank: both zeros alike)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(u16x2, t + rank[i]);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) low[i] = __builtin_elementwise_min(out[i], p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = __builtin_elementwise_sub_sat(out[i], s);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = __builtin_elementwise_max(low[i], out[i]);
-  }
+  __device__ float number(int b) const { return __uint_as_float((uint32_t)(b < middle ? kTiny + middle - b : (kTiny + b - middle) | 0x8000) << 16); }
+  // whether each_bin's 16 bits hold: no number comes round to another's bin
+  __device__ bool usable() const { return middle > -kBelow && middle < kBins - 1; }
+  // whether a token falls into the middle bin at all
+  __device__ bool any_tiny() const { return middle >= 0; }
 };
 
-// f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on are `most`.  Returns whether one of them is tiny.
-// SKIP: f is not called if all numbers of the wave are from `most` on.
+// f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on, NaNs and -infinity are `most`.  Returns whether one of them is
+// tiny.  SKIP: f is not called if all numbers of the wave are from `most` on.  (Step by step for all four words: each step waits for the one
+// before.)
 template <int SIZE, bool SKIP = false, typename F>
 __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4& piece, F f) {
+  constexpr unsigned short kScale = SIZE >= 4 ? 4 : 1, kFar = SIZE >= 4 ? kBins + kBelow + 64 : 0x7fff;      // (farther ones as far: 4 (middle + u) stays below 2^16)
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
-  const u16x2 limit = {(unsigned short)most, (unsigned short)most}, tiny = {(unsigned short)bins.tiny, (unsigned short)bins.tiny};
-  u16x2 two[4], other = {0xffff, 0xffff};
-  bins.of_eight(w, two);
+  const u16x2 limit = u16x2{1, 1} * (unsigned short)(most * kScale), middle = u16x2{1, 1} * (unsigned short)(bins.middle * kScale);
+  u16x2 u[4], sign[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) two[i] = __builtin_elementwise_min(two[i], limit);
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sign[i] = __builtin_bit_cast(u16x2, __builtin_bit_cast(s16x2, w[i]) >> 15);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_elementwise_sub_sat(u[i], u16x2{kTiny, kTiny});
+  const u16x2 least = __builtin_elementwise_min(__builtin_elementwise_min(u[0], u[1]), __builtin_elementwise_min(u[2], u[3]));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sign[i] = (~sign[i] & (unsigned short)(-2 * kScale)) | kScale;      // -SCALE, or SCALE
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_elementwise_min(u[i], u16x2{kFar, kFar});
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = u[i] * sign[i] + middle;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = __builtin_elementwise_min(u[i], limit);
   if (SKIP) {
-    const u16x2 first = __builtin_elementwise_min(__builtin_elementwise_min(two[0], two[1]), __builtin_elementwise_min(two[2], two[3]));
+    const u16x2 first = __builtin_elementwise_min(__builtin_elementwise_min(u[0], u[1]), __builtin_elementwise_min(u[2], u[3]));
     if (!__any(__builtin_bit_cast(uint32_t, first) != __builtin_bit_cast(uint32_t, limit))) return false;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    other = __builtin_elementwise_min(other, two[i] ^ tiny);
-    const uint32_t b = __builtin_bit_cast(uint32_t, two[i] * (unsigned short)SIZE);
-    f(2 * i, b & 0xffff);
-    f(2 * i + 1, b >> 16);
+    const uint32_t b = __builtin_bit_cast(uint32_t, u[i]);
+    f(2 * i, (b & 0xffff) * (SIZE / kScale));
+    f(2 * i + 1, (b >> 16) * (SIZE / kScale));
   }
-  return other[0] == 0 || other[1] == 0;
+  return least[0] == 0 || least[1] == 0;
 }
 
 // f(e) for the tiny numbers of a piece
@@ -400,7 +405,7 @@ __device__ __forceinline__ void each_tiny(const uint4& piece, F f) {
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
   uint32_t mask = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) mask |= ((w[e / 2] >> (e & 1 ? 16 : 0)) & 0x7fff) < (uint32_t)kTiny ? 1u << e : 0;
+  for (int e = 0; e < 8; ++e) mask |= ((w[e / 2] >> (e & 1 ? 16 : 0)) & 0x7fff) <= (uint32_t)kTiny ? 1u << e : 0;
   while (mask) {
     f(__builtin_ctz(mask));
     mask &= mask - 1;
@@ -442,16 +447,16 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   const Weigher weight{(double)most, 369.32993046757463 / (double)heat, sh.powers};
 
   if constexpr (sizeof(T) == 2) {
-    const Bins bins(rank_of(most));
+    const Bins bins(most);
     int border = bins.allowed;                            // kept: bins below the border, and of the border's tokens the first `need`
     uint32_t need = 0;
     uint64_t each = 0;
     int kept = one ? 1 : -1;
     // whether the bins do: a finite maximum, and no weight beyond them
-    bool counted = !one && most < __builtin_inff() && bins.tiny < kBins - 1 && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
+    bool counted = !one && most < __builtin_inff() && bins.usable() && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
     if (one) {
       // the bins of the largest and of everything else
-      if (bins.tiny != 0) {
+      if (bins.middle != 0 && bins.usable()) {
         counted = true;
         border = 0;
         need = 1;
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
         for (int i = 0; i < kMine; ++i) {
           const int b = tid * kMine + i;
           const uint64_t w = n[i] * weight(bins.number(b));
-          mass += b == bins.tiny ? tiny : w;
+          mass += b == bins.middle ? tiny : w;
         }
       }
       const uint64_t my_mass = mass;
@@ -511,14 +516,14 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
         // every wave finds the number on its own
         const int b = sh.index * kMine + lane;
         const uint32_t n = lane >= kMine ? 0 : b == border ? need : b < min(border, bins.n) ? sh.counts[b] : 0;
-        const uint64_t w = n && b != bins.tiny ? weight(bins.number(b)) : 0, here = n == 0 ? 0 : b == bins.tiny ? tiny : n * w;
+        const uint64_t w = n && b != bins.middle ? weight(bins.number(b)) : 0, here = n == 0 ? 0 : b == bins.middle ? tiny : n * w;
         const uint64_t masses = sh.found + wave_scan(here);
         const uint32_t counts = sh.word + wave_scan32(n);
         const int first = __builtin_ctzll(__ballot((round ? (double)masses : (double)counts) >= goal || lane == kMine - 1));
         const uint32_t n_there = __builtin_amdgcn_readlane(n, first), n_before = __builtin_amdgcn_readlane(counts - n, first);
         const uint64_t m_before = lane_of(masses - here, first);
         border = sh.index * kMine + first;
-        if (border == bins.tiny) {
+        if (border == bins.middle) {
           counted = false;
           break;
         }
@@ -532,10 +537,11 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     if (counted && enough > 0) {
       // the first bin whose weight is not enough: near where the logarithm says
       const int b = bins.of((float)((double)most + (double)heat * log((double)least))) - 31 + lane;
-      const bool tiny_first = (double)weight(of_rank(min(bins.top, kTiny - 1))) >= enough, tiny_last = (double)weight(of_rank(1 - kTiny)) >= enough;
-      const bool passes = b < 0 || (b < bins.n && (b == bins.tiny ? tiny_last : (double)weight(bins.number(b)) >= enough));
+      const float tiny_most = 0x1.fep-11f;                 // the largest bf16 below 2^-10
+      const bool tiny_first = (double)weight(fminf(most, tiny_most)) >= enough, tiny_last = (double)weight(-tiny_most) >= enough;
+      const bool passes = b < 0 || (b < bins.n && (b == bins.middle ? tiny_last : (double)weight(bins.number(b)) >= enough));
       const uint64_t passing = __ballot(passes);
-      if (!(passing & 1) || passing >> 63 || (bins.tiny >= 0 && tiny_first != tiny_last)) {
+      if (!(passing & 1) || passing >> 63 || (bins.any_tiny() && tiny_first != tiny_last)) {
         counted = false;
       } else {
         const int limit = lane_of((uint64_t)(uint32_t)b, 0) + __builtin_ctzll(~passing);
@@ -550,14 +556,14 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       // weights of the bins that are kept, as far as they are not 0 (exp(-31.2) 2^44 is below 1/2); a 0 for the border and one for all others
       const int table = max(0, min(min(border, bins.n), bins.of((float)((double)most - 31.2 * (double)heat)) + 2));
       __syncthreads();
-      for (int b = tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != bins.tiny ? weight(bins.number(b)) : 0;
+      for (int b = tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != bins.middle ? weight(bins.number(b)) : 0;
       __syncthreads();
       const uint32_t on_border = need > 0 && border == table ? border * 8 : 0xffff;      // (tokens of a border further down weigh nothing)
       draw(row, sh, a, r, need, each, kept, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
         const bool small = each_bin<8, true>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
           f(e, at == on_border, *reinterpret_cast<const uint64_t*>(reinterpret_cast<const unsigned char*>(sh.weights) + at));
         });
-        if (small && bins.tiny < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
+        if (small && bins.middle < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
       }, [&](const uint4& piece) __attribute__((always_inline)) {
         uint32_t n = 0;
         each_bin<1>(bins, bins.allowed, piece, [&](int, uint32_t b) __attribute__((always_inline)) { n += (int)b < border; });
