@@ -61,8 +61,9 @@ __device__ inline uint32_t key_of(float z) {
   return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 __device__ inline float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
-// a token that may be drawn: neither NaN nor -infinity
-__device__ inline bool allowed(float z) { return z > -__builtin_inff(); }
+// a token that may be drawn: neither NaN nor -infinity.  (A comparison with -infinity itself in a ballot comes out of the compiler as "not
+// equal", which is true of NaN.)
+__device__ inline bool allowed(float z) { return z >= -3.402823466e38f; }
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -245,9 +246,9 @@ __device__ inline uint64_t fewest(uint64_t above, uint64_t each, uint64_t there,
 
 // The draw: weigh(piece, f, g) calls f(e, tie, weight) for each token of a piece: whether it is on the border, and the weight of one above, and
 // g(e, weight) for what weighs more than f was told.  Of the tokens on the border the first `need` weigh `each`.  kept: the number of
-// tokens kept, or -1; then above(piece) counts a lane's tokens above the border.
-template <typename R, typename W, typename N>
-__device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs& a, int r, uint32_t need, uint64_t each, int kept, W weigh, N above) {
+// tokens kept, or -1; then above(piece) counts a lane's tokens above the border.  any(piece): whether the wave has a token to keep.
+template <typename R, typename A, typename W, typename N>
+__device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs& a, int r, uint32_t need, uint64_t each, int kept, A any, W weigh, N above) {
   constexpr int NT = R::kThreads, kParts = NT / 64, kMine = kMaxParts / NT;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), parts = row.n() * kParts;
   const bool count = a.kept && kept < 0;
@@ -255,12 +256,14 @@ __device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs&
   row.pieces([&](int c, const uint4& p) __attribute__((always_inline)) {
     uint64_t sum = 0;
     uint32_t ties = 0;
-    weigh(p, [&](int, bool tie, uint64_t w) __attribute__((always_inline)) {
-      sum += w;
-      ties += __popcll(__ballot(tie));
-    }, [&](int, uint64_t w) __attribute__((always_inline)) { sum += w; });
-    if (count) number += above(p);
-    sum = wave_scan(sum);
+    if (any(p)) {
+      weigh(p, [&](int, bool tie, uint64_t w) __attribute__((always_inline)) {
+        sum += w;
+        ties += __popcll(__ballot(tie));
+      }, [&](int, uint64_t w) __attribute__((always_inline)) { sum += w; });
+      if (count) number += above(p);
+      sum = wave_scan(sum);
+    }
     if (lane == 63) {
       sh.part.sum[c * kParts + wave] = sum;
       sh.part.ties[c * kParts + wave] = ties;
@@ -363,9 +366,8 @@ struct Bins {
 };
 
 // f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on, NaNs and -infinity are `most`.  Returns whether one of them is
-// tiny.  SKIP: f is not called if all numbers of the wave are from `most` on.  (Step by step for all four words: each step waits for the one
-// before.)
-template <int SIZE, bool SKIP = false, typename F>
+// tiny.  (Step by step for all four words: each step waits for the one before.)
+template <int SIZE, typename F>
 __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4& piece, F f) {
   constexpr unsigned short kScale = SIZE >= 4 ? 4 : 1, kFar = SIZE >= 4 ? kBins + kBelow + 64 : 0x7fff;      // (farther ones as far: 4 (middle + u) stays below 2^16)
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
@@ -386,10 +388,6 @@ __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4
   for (int i = 0; i < 4; ++i) u[i] = u[i] * sign[i] + middle;
 #pragma unroll
   for (int i = 0; i < 4; ++i) u[i] = __builtin_elementwise_min(u[i], limit);
-  if (SKIP) {
-    const u16x2 first = __builtin_elementwise_min(__builtin_elementwise_min(u[0], u[1]), __builtin_elementwise_min(u[2], u[3]));
-    if (!__any(__builtin_bit_cast(uint32_t, first) != __builtin_bit_cast(uint32_t, limit))) return false;
-  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t b = __builtin_bit_cast(uint32_t, u[i]);
@@ -428,11 +426,25 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   if (tid < 256) sh.powers[tid] = exp2(tid / 256.0);
 
   float most = -__builtin_inff();
-  row.template each<8>([&](float z) __attribute__((always_inline)) { most = fmaxf(most, z); });
+  const bool unfiltered = a.kept && !(k > 0 && k < a.vocab) && !(p < 1.f) && !(least > 0.f);      // then all tokens are kept: how many?
+  uint32_t number = 0;
+  row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < Row<T, NT>::kVec; ++e) most = fmaxf(most, Row<T, NT>::number(piece, e));
+    if (unfiltered) {
+#pragma unroll
+      for (int e = 0; e < Row<T, NT>::kVec; ++e) number += __popcll(__ballot(allowed(Row<T, NT>::number(piece, e))));
+    }
+  });
   most = wave_max(most);
-  if (lane == 0) sh.most[wave] = most;
+  if (lane == 0) {
+    sh.most[wave] = most;
+    sh.numbers[wave] = number;
+  }
   __syncthreads();
   most = wave_max(lane < kWaves ? sh.most[lane] : -__builtin_inff());
+  int kept = -1;
+  if (unfiltered) kept = __builtin_amdgcn_readlane(wave_scan32(lane < kWaves ? sh.numbers[lane] : 0), 63);
   if (!allowed(most)) {
     if (tid == 0) {
       a.token[r] = 0;
@@ -441,7 +453,9 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     }
     return;
   }
-  const bool one = !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f;       // the first of the order alone
+  // the first of the order alone
+  const bool one = !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f;
+  if (one) kept = 1;
   const bool by_count = k > 0 && k < a.vocab && !one, by_mass = p < 1.f && !one;
   const double enough = least > 0.f && !one ? (double)least * kUnit : 0.0;
   const Weigher weight{(double)most, 369.32993046757463 / (double)heat, sh.powers};
@@ -451,7 +465,6 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     int border = bins.allowed;                            // kept: bins below the border, and of the border's tokens the first `need`
     uint32_t need = 0;
     uint64_t each = 0;
-    int kept = one ? 1 : -1;
     // whether the bins do: a finite maximum, and no weight beyond them
     bool counted = !one && most < __builtin_inff() && bins.usable() && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
     if (one) {
@@ -559,8 +572,14 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       for (int b = tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != bins.middle ? weight(bins.number(b)) : 0;
       __syncthreads();
       const uint32_t on_border = need > 0 && border == table ? border * 8 : 0xffff;      // (tokens of a border further down weigh nothing)
-      draw(row, sh, a, r, need, each, kept, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
-        const bool small = each_bin<8, true>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
+      // where what is kept is positive, a wave looks at its largest number first (positive bf16 numbers are in the order of their bits)
+      const int lowest = table < bins.middle ? (int)(__float_as_uint(bins.number(table)) >> 16) : -0x8000;
+      draw(row, sh, a, r, need, each, kept, [&](const uint4& p) __attribute__((always_inline)) {
+        const auto two = [](uint32_t w) { return __builtin_bit_cast(s16x2, w); };
+        const s16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(p.x), two(p.y)), __builtin_elementwise_max(two(p.z), two(p.w)));
+        return (bool)__any(max(m[0], m[1]) >= lowest);
+      }, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
+        const bool small = each_bin<8>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
           f(e, at == on_border, *reinterpret_cast<const uint64_t*>(reinterpret_cast<const unsigned char*>(sh.weights) + at));
         });
         if (small && bins.middle < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
@@ -574,21 +593,17 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   }
 
   // the border's key digit by digit: by count, then by mass
+  if (!one && !unfiltered) kept = -1;
   constexpr int kSlow = sizeof(T) == 2 ? 1 : 4;           // (of bf16 rows few come here)
   uint32_t border = one ? key_of(most) : 0x007fffffu;     // (-infinity's)
-  uint64_t need = one, each = one ? (uint64_t)kUnit : 0;
+  uint32_t need = one;
+  uint64_t each = one ? (uint64_t)kUnit : 0, over = 0;
   auto inside = [&](uint32_t key, float z) __attribute__((always_inline)) { return allowed(z) && key >= border; };
 #pragma unroll 1
   for (int round = 0; round < 2; ++round) {
     if (!(round ? by_mass : by_count)) continue;
-    uint64_t total = 0;
-    row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
-      const uint32_t key = key_of(z);
-      if (allowed(z) && key > border) total += round ? weight(z) : 1;
-    });
-    before_me<NT>(total, sh, total);
-    if (!round && (uint64_t)k >= total) continue;
-    const double goal = round ? (double)p * (double)(total + need * each) : (double)k;
+    double goal = 0;
+    bool none = false;                                    // no border: all tokens are kept
     uint32_t prefix = 0;
     uint64_t above = 0;
     int shift = 32;
@@ -610,6 +625,12 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       uint64_t sum = 0, whole;
       for (int i = 0; i < kMine; ++i) sum += top - i >= 0 ? sh.digits[top - i] : 0;
       uint64_t run = above + before_me<NT>(sum, sh, whole);
+      if (step == 0) {
+        // (of tokens with the border's key of the first round the digits hold all: `over` too many)
+        none = !round && (uint64_t)k >= whole;
+        if (none) break;
+        goal = round ? (double)p * (double)(whole - over) : (double)k;
+      }
       if ((double)run < goal && (double)(run + sum) >= goal) {
         int digit = top;
         while ((double)(run + sh.digits[digit]) < goal) run += sh.digits[digit--];
@@ -621,9 +642,12 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       above = sh.found;
       prefix = sh.word;
     }
+    if (none) continue;
     // (tokens with the border's key of the first round: `need` of them, whatever the digits have added up)
     const uint64_t w = weight(of_key(prefix)), unit = round ? w : 1;
-    need = fewest(above, unit, prefix == border ? need : unit ? sh.found2 / unit : 1, goal);
+    const uint64_t there = unit ? sh.found2 / unit : 1;
+    need = (uint32_t)fewest(above, unit, prefix == border ? need : there, goal);
+    over = (there - need) * w;
     each = w;
     border = prefix;
     __syncthreads();
@@ -638,7 +662,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
       need = 0;
     }
   }
-  draw(row, sh, a, r, need, each, one ? 1 : -1, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
+  draw(row, sh, a, r, need, each, kept, [](const uint4&) { return true; }, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < Row<T, NT>::kVec; ++e) {
       const float z = Row<T, NT>::number(piece, e);
