@@ -1,9 +1,9 @@
 // Low-rank adapters of many requests beside a shared projection: y[r] = sum_s base[s][r] + scale_a B_a (A_a x[r]), a = row_adapter[r].
 //
-// Two launches: h[r] = A_a x[r] in fp32 (a reduction over k: workgroups along it, partial sums in the workspace), then scale h B^T beside
-// the base.  A workgroup takes 16 rows.  One of its products serves all of them that have the same adapter, its leader being the
-// first of these; every row's results come from the product of its own adapter, so no row's numbers meet another's weights.
-// The second product keeps h whole: scale h is split into three bf16 parts of 8 bits each, which the matrix cores take side by side.
+// Two launches: h[r] = scale_a A_a x[r] in fp32 (a reduction over k by the waves of a workgroup), then h B^T beside the base.  Rows go
+// sixteen at a time.  One product serves all of them that have the same adapter, the first of these rows being its leader; every row takes
+// its results from the product of its own adapter, so no row's numbers meet another's weights.  The second product keeps h whole:
+// it is split into three bf16 parts of 8 bits each, which the matrix cores take side by side.
 //
 // The bank:
 //   head  [n_slots] scale fp32, [n_slots] rank i32 (0: empty)
@@ -11,12 +11,15 @@
 //         B: [n / 16][rank tiles][32 lanes][8]         lane l output l % 16, ranks 8 (l / 16) .. + 7 of 16; the other half of a 32-deep
 //                                                      product takes the same numbers again, for another part of h
 // Ranks, inputs and outputs past the matrices are zeros.
+// h between the launches: [row][rank tiles][high, middle, low part, zeros][16]
 #include "sl_common.h"
 
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x4_unaligned __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kRows = 16;
 
@@ -68,94 +71,162 @@ __device__ inline int adapter_of_row(const Bank& bank, const int32_t* row_adapte
   return a >= 0 && a < bank.n_slots && bank.ranks()[a] > 0 ? a : -1;
 }
 
-// h[split][row][ranks] for the rows of one adapter among 16: workgroup (row, split, rank tile), if the row is the first of its adapter
-__global__ __launch_bounds__(256) void adapters_down_kernel(Bank bank, const bf16_t* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
-                                                            int splits, float* h) {
-  const int m = min(*m_dev, m_upper), row = blockIdx.x;
-  if (row >= m) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r0 = row & ~(kRows - 1), r = r0 + (lane & 15);
-  const int own = adapter_of_row(bank, row_adapter, r, m), a = __builtin_amdgcn_readlane(own, row - r0);
-  if (a < 0 || __builtin_ctzll(__ballot(own == a)) != row - r0) return;
-  const int tile = blockIdx.z;
-  if (tile * 16 >= bank.ranks()[a]) return;
-  const int blocks = (bank.k + 31) / 32, b0 = (int)((int64_t)blocks * blockIdx.y / splits), b1 = (int)((int64_t)blocks * (blockIdx.y + 1) / splits);
-  const bf16x8* w = (const bf16x8*)bank.a_of(a) + (size_t)tile * blocks * 64;
-  const bf16_t* xr = x + (size_t)min(r, m - 1) * bank.k;
-  f32x4 acc = {};
-  for (int b = b0 + wave; b < b1; b += 4) {
-    const int c = b * 32 + (lane >> 4) * 8;
-    bf16x8 v = {};
-    if (c < bank.k) v = *(const bf16x8*)(xr + c);
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[(size_t)b * 64 + lane], v, acc, 0, 0, 0);
-  }
-  __shared__ f32x4 part[4][64];
-  part[wave][lane] = acc;
-  __syncthreads();
-  if (wave == 0 && own == a) {
-    const f32x4 sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-    *(f32x4*)(h + ((size_t)blockIdx.y * m_upper + r) * bank.rank_tiles * 16 + tile * 16 + (lane >> 4) * 4) = sum;
-  }
-}
-
+// The three parts of v, of 8 bits each
 __device__ inline void split3(float v, bf16_t& a, bf16_t& b, bf16_t& c) {
   a = (bf16_t)v;
   b = (bf16_t)(v - (float)a);
   c = (bf16_t)(v - (float)a - (float)b);
 }
 
-// 16 rows, 64 columns a workgroup
-template <typename T>
-__global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const float* h, int h_splits, const int32_t* row_adapter, const int32_t* m_dev,
-                                                          int m_upper, const float* base, int splits, T* y) {
+// h for the rows of one adapter among 16 and RT rank tiles: workgroup (row, tiles), if the row is the first of its adapter
+template <int RT>
+__global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf16_t* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
+                                                             bf16_t* h) {
+  constexpr int kWaves = 16, U = RT == 4 ? 2 : 4;         // blocks of 32 inputs that a wave asks for at once
+  const int m = min(*m_dev, m_upper), row = blockIdx.x;
+  if (row >= m) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = row & ~(kRows - 1), r = r0 + (lane & 15);
+  const int own = adapter_of_row(bank, row_adapter, r, m), a = __builtin_amdgcn_readlane(own, row - r0);
+  if (a < 0 || __builtin_ctzll(__ballot(own == a)) != row - r0) return;
+  const int tile = blockIdx.y * RT, tiles = (bank.ranks()[a] + 15) / 16;
+  if (tile >= tiles) return;
+  const int blocks = (bank.k + 31) / 32, b0 = blocks * wave / kWaves, b1 = blocks * (wave + 1) / kWaves;
+  const bf16x8* w[RT];                                    // (a tile past the last is read as the last and not stored)
+#pragma unroll
+  for (int t = 0; t < RT; ++t) w[t] = (const bf16x8*)bank.a_of(a) + (size_t)min(tile + t, tiles - 1) * blocks * 64 + lane;
+  const bf16_t* xr = x + (size_t)min(r, m - 1) * bank.k + (lane >> 4) * 8;
+  f32x4 acc[RT] = {};
+  for (int b = b0; b < b1; b += U) {
+    bf16x8 v[U], a8[U][RT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = min(b + u, b1 - 1);
+      v[u] = bf16x8{};
+      if (b + u < b1 && at * 32 + (lane >> 4) * 8 < bank.k) v[u] = *(const bf16x8*)(xr + at * 32);      // (zeros for a block too many)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) a8[u][t] = w[t][(size_t)at * 64];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8[u][t], v[u], acc[t], 0, 0, 0);
+  }
+  __shared__ __attribute__((aligned(16))) float part[kWaves][RT][16][16];      // [..][row][rank]
+#pragma unroll
+  for (int t = 0; t < RT; ++t) *(f32x4*)&part[wave][t][lane & 15][(lane >> 4) * 4] = acc[t];
+  __syncthreads();
+  const float scale = bank.scales()[a];
+  for (int i = threadIdx.x; i < RT * 256; i += 1024) {
+    const int t = i / 256, at = i / 16 % 16, rank = i % 16;
+    const int to = r0 + at, its = __builtin_amdgcn_ds_bpermute(at * 4, own);      // (whole waves ask)
+    if (tile + t >= tiles || to >= m || its != a) continue;
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) sum += part[v][t][at][rank];
+    bf16_t* out = h + (((size_t)to * bank.rank_tiles + tile + t) * 4) * 16 + rank;
+    split3(scale * sum, out[0], out[16], out[32]);
+    out[48] = (bf16_t)0.f;
+  }
+}
+
+// 16 rows and 16 CT columns a wave.  The products of one adapter and rank tile are a step; D steps are asked for at once.
+template <typename T, int CT, int D>
+__global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_t* h, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
+                                                          const float* base, int splits, T* y) {
   const int m = min(*m_dev, m_upper), r0 = blockIdx.y * kRows;
   if (r0 >= m) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = r0 + (lane & 15), tile_n = blockIdx.x * 4 + wave;
-  if (tile_n * 16 >= bank.n) return;
-  const int own = adapter_of_row(bank, row_adapter, r, m);
-  f32x4 y4 = {};
-  uint64_t todo = __ballot(own >= 0) & 0xffff;
-  while (todo) {
-    const int a = __builtin_amdgcn_readlane(own, __builtin_ctzll(todo));
-    const uint64_t rows = __ballot(own == a);
-    todo &= ~rows;
-    const int rank = bank.ranks()[a], tiles = (rank + 15) / 16;
-    const float scale = bank.scales()[a];
-    const bf16x8* w = (const bf16x8*)bank.b_of(a) + (size_t)tile_n * tiles * 32 + (lane & 31);
-    f32x4 acc = {};
-    for (int t = 0; t < tiles; ++t) {
-      bf16x8 first = {}, second = {};
-      if (own == a) {
-        float v[8] = {};
-        for (int s = 0; s < h_splits; ++s) {
-          const float* from = h + ((size_t)s * m_upper + r) * bank.rank_tiles * 16 + t * 16 + (lane >> 4 & 1) * 8;
-          for (int e = 0; e < 8; ++e) v[e] += from[e];
-        }
-        for (int e = 0; e < 8; ++e) {
-          bf16_t p0, p1, p2;
-          split3(scale * v[e], p0, p1, p2);
-          first[e] = lane < 32 ? p0 : p1;
-          second[e] = lane < 32 ? p2 : (bf16_t)0.f;
-        }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), rr = min(r, m - 1);
+  const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT;
+  if (first >= tiles_n) return;
+  const int own = adapter_of_row(bank, row_adapter, r, m), my_tiles = own >= 0 ? (bank.ranks()[own] + 15) / 16 : 0;
+  const bool wide = bank.n % 4 == 0;                      // four columns of a row at once
+  f32x4 sum[CT], out[CT] = {};
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int col = (first + c) * 16 + (lane >> 4) * 4;
+    sum[c] = f32x4{};
+    if (!base || col >= bank.n) continue;
+    for (int s = 0; s < splits; ++s) {
+      const float* from = base + ((size_t)s * m_upper + rr) * bank.n + col;
+      if (wide) {
+        sum[c] += *(const f32x4_unaligned*)from;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + e < bank.n) sum[c][e] += from[e];
       }
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[(size_t)t * 32], second, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[(size_t)t * 32], first, acc, 0, 0, 0);
     }
-    if (own == a) y4 = acc;
+  }
+  const bf16_t* hr = h + (size_t)rr * bank.rank_tiles * 64 + (lane >> 4) * 8;
+  uint64_t todo = __ballot(own >= 0) & 0xffff;
+  int a = -1, t = 0, tiles = 0;                           // the step that comes next; of a row's own adapter the numbers count, whatever h holds otherwise
+  f32x4 acc[CT] = {};
+  auto next = [&]() {
+    if (++t < tiles) return;
+    t = 0;
+    if (todo) {
+      const int row = __builtin_ctzll(todo);
+      a = __builtin_amdgcn_readlane(own, row);
+      tiles = __builtin_amdgcn_readlane(my_tiles, row);
+      todo &= ~__ballot(own == a);
+    } else {
+      a = -1;
+      tiles = 0;
+    }
+  };
+  next();
+  while (a >= 0) {
+    bf16x8 hi[D], lo[D], w[D][CT];
+    int step_a[D];
+    bool starts[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      step_a[d] = a;
+      starts[d] = t == 0;
+      if (a < 0) continue;
+      hi[d] = *(const bf16x8*)(hr + t * 64);
+      lo[d] = *(const bf16x8*)(hr + t * 64 + 32);
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+        w[d][c] = *((const bf16x8*)bank.b_of(a) + ((size_t)min(first + c, tiles_n - 1) * tiles + t) * 32 + (lane & 31));
+      next();
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      if (step_a[d] < 0) break;
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        const f32x4 zero = {};
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[d][c], lo[d], starts[d] ? zero : acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[d][c], hi[d], acc[c], 0, 0, 0);
+        if (own == step_a[d]) out[c] = acc[c];
+      }
+    }
   }
   if (r >= m) return;
-  for (int e = 0; e < 4; ++e) {
-    const int c = tile_n * 16 + (lane >> 4) * 4 + e;
-    if (c >= bank.n) break;
-    float sum = 0.f;
-    for (int s = 0; base && s < splits; ++s) sum += base[((size_t)s * m_upper + r) * bank.n + c];
-    st<T>::stv(y + (size_t)r * bank.n + c, sum + y4[e]);
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int col = (first + c) * 16 + (lane >> 4) * 4;
+    T* to = y + (size_t)r * bank.n + col;
+    const f32x4 v = own >= 0 ? sum[c] + out[c] : sum[c];
+    if (wide && col < bank.n) {
+      if constexpr (sizeof(T) == 2) {
+        bf16x4_unaligned b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = (bf16_t)v[e];
+        *(bf16x4_unaligned*)to = b;
+      } else {
+        *(f32x4_unaligned*)to = v;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (col + e < bank.n) st<T>::stv(to + e, v[e]);
+    }
   }
 }
 
 Bank bank_of(const sl_adapters* ad) { return Bank{(unsigned char*)ad->bank, ad->n_slots, sl_cdiv(ad->max_rank, 16), ad->n, ad->k}; }
-
-// Workgroups along k
-int down_splits(int k) { return min(8, sl_cdiv(k, 512)); }
 
 }  // namespace
 
@@ -178,24 +249,27 @@ int slk_adapters_pack(hipStream_t s, const sl_adapters* ad, int slot, int rank, 
   return SL_OK;
 }
 
-size_t slk_adapters_workspace_bytes(const sl_adapters* ad, int m_upper) {
-  return (size_t)down_splits(ad->k) * m_upper * sl_cdiv(ad->max_rank, 16) * 16 * 4;
-}
+size_t slk_adapters_workspace_bytes(const sl_adapters* ad, int m_upper) { return (size_t)m_upper * sl_cdiv(ad->max_rank, 16) * 128; }
 
 int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                          const float* base, int splits, float* y_f32, void* y_bf16, void* workspace) {
   const Bank bank = bank_of(ad);
-  const int h_splits = down_splits(ad->k);
-  hipLaunchKernelGGL(adapters_down_kernel, dim3(m_upper, h_splits, bank.rank_tiles), dim3(256), 0, s, bank, (const bf16_t*)x, row_adapter, m_dev,
-                     m_upper, h_splits, (float*)workspace);
+  bf16_t* h = (bf16_t*)workspace;
+  // rank tiles a workgroup: as many as leave one for each CU (each reads the rows again)
+  const int tiles = bank.rank_tiles, groups = sl_cdiv(m_upper, kRows);
+#define DOWN_RUN(RT) \
+  hipLaunchKernelGGL(adapters_down_kernel<RT>, dim3(m_upper, sl_cdiv(tiles, RT)), dim3(1024), 0, s, bank, (const bf16_t*)x, row_adapter, m_dev, m_upper, h)
+  if (tiles >= 4 && groups * sl_cdiv(tiles, 4) >= 192) DOWN_RUN(4);
+  else if (tiles >= 2 && groups * sl_cdiv(tiles, 2) >= 192) DOWN_RUN(2);
+  else DOWN_RUN(1);
+#undef DOWN_RUN
   SL_LAUNCH_CHECK();
-  const dim3 grid(sl_cdiv(ad->n, 64), sl_cdiv(m_upper, kRows));
-  if (y_f32)
-    hipLaunchKernelGGL((adapters_up_kernel<float>), grid, dim3(256), 0, s, bank, (const float*)workspace, h_splits, row_adapter, m_dev, m_upper, base,
-                       splits, y_f32);
-  else
-    hipLaunchKernelGGL((adapters_up_kernel<bf16_t>), grid, dim3(256), 0, s, bank, (const float*)workspace, h_splits, row_adapter, m_dev, m_upper, base,
-                       splits, (bf16_t*)y_bf16);
+#define UP_RUN(T, CT, D, Y) \
+  hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256), 0, s, bank, h, row_adapter, m_dev, m_upper, \
+                     base, splits, Y)
+  if (y_f32) UP_RUN(float, 2, 4, y_f32);
+  else UP_RUN(bf16_t, 2, 4, (bf16_t*)y_bf16);
+#undef UP_RUN
   SL_LAUNCH_CHECK();
   return SL_OK;
 }
