@@ -78,54 +78,76 @@ __device__ inline void split3(float v, bf16_t& a, bf16_t& b, bf16_t& c) {
   c = (bf16_t)(v - (float)a - (float)b);
 }
 
-// h for the rows of one adapter among 16 and RT rank tiles: workgroup (row, tiles), if the row is the first of its adapter
-template <int RT>
+// h for 16 rows and RT rank tiles: workgroup (rows, place, tiles) takes the adapters of these rows, every gridDim.y-th of them, one after another.
+//
+// The rows pass through LDS, 512 inputs at a time: a wave loads 1 KiB of one row, and takes 32 inputs of all sixteen as an operand.  (An
+// operand loaded from row-major memory is 64 bytes of each of sixteen rows that lie a power of two apart.)  Pieces of 16 bytes that would
+// meet in one bank are kept apart by an exclusive or of their row with their place.  P chunks are on their way.
+template <int RT, int P>
 __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf16_t* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                                                              bf16_t* h) {
-  constexpr int kWaves = 16, U = RT == 4 ? 2 : 4;         // blocks of 32 inputs that a wave asks for at once
-  const int m = min(*m_dev, m_upper), row = blockIdx.x;
-  if (row >= m) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = row & ~(kRows - 1), r = r0 + (lane & 15);
-  const int own = adapter_of_row(bank, row_adapter, r, m), a = __builtin_amdgcn_readlane(own, row - r0);
-  if (a < 0 || __builtin_ctzll(__ballot(own == a)) != row - r0) return;
-  const int tile = blockIdx.y * RT, tiles = (bank.ranks()[a] + 15) / 16;
-  if (tile >= tiles) return;
-  const int blocks = (bank.k + 31) / 32, b0 = blocks * wave / kWaves, b1 = blocks * (wave + 1) / kWaves;
-  const bf16x8* w[RT];                                    // (a tile past the last is read as the last and not stored)
+  constexpr int kWaves = 16, kChunk = 512;
+  __shared__ __attribute__((aligned(16))) union {
+    unsigned char rows[2][kRows * kChunk * 2];
+    float part[kWaves][RT][16][16];                       // [..][row][rank]
+  } sh;
+  const int m = min(*m_dev, m_upper), r0 = blockIdx.x * kRows;
+  if (r0 >= m) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), q = lane >> 4;
+  const int own = adapter_of_row(bank, row_adapter, r, m), my_tiles = own >= 0 ? (bank.ranks()[own] + 15) / 16 : 0;
+  const float my_scale = own >= 0 ? bank.scales()[own] : 0.f;
+  const int tile = blockIdx.z * RT, blocks = (bank.k + 31) / 32, chunks = (bank.k + kChunk - 1) / kChunk;
+  const bf16_t* xr = x + (size_t)min(r0 + wave, m - 1) * bank.k + lane * 8;
+  unsigned char* put = &sh.rows[0][wave * 1024 + (lane ^ wave) * 16];
+  const unsigned char* get = &sh.rows[0][(lane & 15) * 1024 + ((wave * 4 + q) ^ (lane & 15)) * 16];
+  uint64_t todo = __ballot(own >= 0) & 0xffff;
+  for (int place = 0; todo; ++place) {
+    const int leader = __builtin_ctzll(todo), a = __builtin_amdgcn_readlane(own, leader), tiles = __builtin_amdgcn_readlane(my_tiles, leader);
+    const uint64_t its = __ballot(own == a);
+    todo &= ~its;
+    if (place % gridDim.y != blockIdx.y || tile >= tiles) continue;
+    const bf16x8* w[RT];                                  // (a tile past the last is read as the last and not stored)
 #pragma unroll
-  for (int t = 0; t < RT; ++t) w[t] = (const bf16x8*)bank.a_of(a) + (size_t)min(tile + t, tiles - 1) * blocks * 64 + lane;
-  const bf16_t* xr = x + (size_t)min(r, m - 1) * bank.k + (lane >> 4) * 8;
-  f32x4 acc[RT] = {};
-  for (int b = b0; b < b1; b += U) {
-    bf16x8 v[U], a8[U][RT];
+    for (int t = 0; t < RT; ++t) w[t] = (const bf16x8*)bank.a_of(a) + ((size_t)min(tile + t, tiles - 1) * blocks + wave) * 64 + lane;
+    bf16x8 xs[P], ws[P][RT];
+    auto ask = [&](int p, int c) __attribute__((always_inline)) {
+      xs[p] = bf16x8{};                                   // (inputs past the last are zeros, and the last block is read for those behind it)
+      if (c * kChunk + lane * 8 < bank.k) xs[p] = *(const bf16x8*)(xr + c * kChunk);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = min(b + u, b1 - 1);
-      v[u] = bf16x8{};
-      if (b + u < b1 && at * 32 + (lane >> 4) * 8 < bank.k) v[u] = *(const bf16x8*)(xr + at * 32);      // (zeros for a block too many)
+      for (int t = 0; t < RT; ++t) ws[p][t] = w[t][(ptrdiff_t)min(c * 16, blocks - 1 - wave) * 64];
+    };
+    f32x4 acc[RT] = {};
 #pragma unroll
-      for (int t = 0; t < RT; ++t) a8[u][t] = w[t][(size_t)at * 64];
+    for (int p = 0; p < P; ++p)
+      if (p < chunks) ask(p, p);
+    for (int c0 = 0; c0 < chunks; c0 += P)
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int c = c0 + p;
+        if (c >= chunks) break;
+        *(bf16x8*)(put + (c & 1) * (kRows * kChunk * 2)) = xs[p];
+        __syncthreads();
+        const bf16x8 v = *(const bf16x8*)(get + (c & 1) * (kRows * kChunk * 2));
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[p][t], v, acc[t], 0, 0, 0);
+        if (c + P < chunks) ask(p, c + P);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *(f32x4*)&sh.part[wave][t][lane & 15][q * 4] = acc[t];
+    __syncthreads();
+    const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_scale), leader));
+    for (int i = threadIdx.x; i < RT * 256; i += 1024) {
+      const int t = i / 256, at = i / 16 % 16, rank = i % 16;
+      if (tile + t >= tiles || !(its >> at & 1)) continue;
+      float sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) sum += sh.part[v][t][at][rank];
+      bf16_t* out = h + (((size_t)(r0 + at) * bank.rank_tiles + tile + t) * 4) * 16 + rank;
+      split3(scale * sum, out[0], out[16], out[32]);
+      out[48] = (bf16_t)0.f;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a8[u][t], v[u], acc[t], 0, 0, 0);
-  }
-  __shared__ __attribute__((aligned(16))) float part[kWaves][RT][16][16];      // [..][row][rank]
-#pragma unroll
-  for (int t = 0; t < RT; ++t) *(f32x4*)&part[wave][t][lane & 15][(lane >> 4) * 4] = acc[t];
-  __syncthreads();
-  const float scale = bank.scales()[a];
-  for (int i = threadIdx.x; i < RT * 256; i += 1024) {
-    const int t = i / 256, at = i / 16 % 16, rank = i % 16;
-    const int to = r0 + at, its = __builtin_amdgcn_ds_bpermute(at * 4, own);      // (whole waves ask)
-    if (tile + t >= tiles || to >= m || its != a) continue;
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) sum += part[v][t][at][rank];
-    bf16_t* out = h + (((size_t)to * bank.rank_tiles + tile + t) * 4) * 16 + rank;
-    split3(scale * sum, out[0], out[16], out[32]);
-    out[48] = (bf16_t)0.f;
+    __syncthreads();
   }
 }
 
@@ -255,13 +277,18 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
                          const float* base, int splits, float* y_f32, void* y_bf16, void* workspace) {
   const Bank bank = bank_of(ad);
   bf16_t* h = (bf16_t*)workspace;
-  // rank tiles a workgroup: as many as leave one for each CU (each reads the rows again)
+  // rank tiles a workgroup: as many as leave one for each CU (each reads the rows again); adapters of sixteen rows side by side: all of them
+  // while that is no more than a few workgroups for each CU
   const int tiles = bank.rank_tiles, groups = sl_cdiv(m_upper, kRows);
-#define DOWN_RUN(RT) \
-  hipLaunchKernelGGL(adapters_down_kernel<RT>, dim3(m_upper, sl_cdiv(tiles, RT)), dim3(1024), 0, s, bank, (const bf16_t*)x, row_adapter, m_dev, m_upper, h)
-  if (tiles >= 4 && groups * sl_cdiv(tiles, 4) >= 192) DOWN_RUN(4);
-  else if (tiles >= 2 && groups * sl_cdiv(tiles, 2) >= 192) DOWN_RUN(2);
-  else DOWN_RUN(1);
+#define DOWN_RUN(RT, P)                                                                                                            \
+  do {                                                                                                                             \
+    const int z = sl_cdiv(tiles, RT), side = max(2, min(16, 1024 / (groups * z)));                                                   \
+    hipLaunchKernelGGL((adapters_down_kernel<RT, P>), dim3(groups, min(side, m_upper), z), dim3(1024), 0, s, bank, (const bf16_t*)x,    \
+                       row_adapter, m_dev, m_upper, h);                                                                              \
+  } while (0)
+  if (tiles >= 4 && groups * sl_cdiv(tiles, 4) >= 192) DOWN_RUN(4, 2);
+  else if (tiles >= 2 && groups * sl_cdiv(tiles, 2) >= 192) DOWN_RUN(2, 4);
+  else DOWN_RUN(1, 4);
 #undef DOWN_RUN
   SL_LAUNCH_CHECK();
 #define UP_RUN(T, CT, D, Y) \
