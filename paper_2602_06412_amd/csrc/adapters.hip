@@ -82,15 +82,13 @@ __device__ inline void split3(float v, bf16_t& a, bf16_t& b, bf16_t& c) {
 //
 // The rows pass through LDS, 512 inputs at a time: a wave loads 1 KiB of one row, and takes 32 inputs of all sixteen as an operand.  (An
 // operand loaded from row-major memory is 64 bytes of each of sixteen rows that lie a power of two apart.)  Pieces of 16 bytes that would
-// meet in one bank are kept apart by an exclusive or of their row with their place.  P chunks are on their way.
+// meet in one bank are kept apart by an exclusive or of their row with their place.  P chunks share a barrier, and the next P are on their way.
 template <int RT, int P>
 __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf16_t* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                                                              bf16_t* h) {
-  constexpr int kWaves = 16, kChunk = 512;
-  __shared__ __attribute__((aligned(16))) union {
-    unsigned char rows[2][kRows * kChunk * 2];
-    float part[kWaves][RT][16][16];                       // [..][row][rank]
-  } sh;
+  constexpr int kWaves = 16, kChunk = 512, kChunkBytes = kRows * kChunk * 2;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];      // rows [2][P][16][512], and after them part [kWaves][RT][row][rank]
+  auto part = reinterpret_cast<float(*)[RT][16][16]>(lds);
   const int m = min(*m_dev, m_upper), r0 = blockIdx.x * kRows;
   if (r0 >= m) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), q = lane >> 4;
@@ -98,8 +96,8 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
   const float my_scale = own >= 0 ? bank.scales()[own] : 0.f;
   const int tile = blockIdx.z * RT, blocks = (bank.k + 31) / 32, chunks = (bank.k + kChunk - 1) / kChunk;
   const bf16_t* xr = x + (size_t)min(r0 + wave, m - 1) * bank.k + lane * 8;
-  unsigned char* put = &sh.rows[0][wave * 1024 + (lane ^ wave) * 16];
-  const unsigned char* get = &sh.rows[0][(lane & 15) * 1024 + ((wave * 4 + q) ^ (lane & 15)) * 16];
+  unsigned char* put = lds + wave * 1024 + (lane ^ wave) * 16;
+  const unsigned char* get = lds + (lane & 15) * 1024 + ((wave * 4 + q) ^ (lane & 15)) * 16;
   uint64_t todo = __ballot(own >= 0) & 0xffff;
   for (int place = 0; todo; ++place) {
     const int leader = __builtin_ctzll(todo), a = __builtin_amdgcn_readlane(own, leader), tiles = __builtin_amdgcn_readlane(my_tiles, leader);
@@ -118,23 +116,29 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
     };
     f32x4 acc[RT] = {};
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      if (p < chunks) ask(p, p);
-    for (int c0 = 0; c0 < chunks; c0 += P)
+    for (int p = 0; p < P; ++p) ask(p, p);
+    for (int c0 = 0, side = 0; c0 < chunks; c0 += P, side ^= P * kChunkBytes) {
+      bf16x8 now[P][RT];
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const int c = c0 + p;
-        if (c >= chunks) break;
-        *(bf16x8*)(put + (c & 1) * (kRows * kChunk * 2)) = xs[p];
-        __syncthreads();
-        const bf16x8 v = *(const bf16x8*)(get + (c & 1) * (kRows * kChunk * 2));
+        *(bf16x8*)(put + side + p * kChunkBytes) = xs[p];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ws[p][t], v, acc[t], 0, 0, 0);
-        if (c + P < chunks) ask(p, c + P);
+        for (int t = 0; t < RT; ++t) now[p][t] = ws[p][t];
       }
+      if (c0 + P < chunks)
+#pragma unroll
+        for (int p = 0; p < P; ++p) ask(p, c0 + P + p);
+      __syncthreads();
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const bf16x8 v = *(const bf16x8*)(get + side + p * kChunkBytes);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now[p][t], v, acc[t], 0, 0, 0);
+      }
+    }
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < RT; ++t) *(f32x4*)&sh.part[wave][t][lane & 15][q * 4] = acc[t];
+    for (int t = 0; t < RT; ++t) *(f32x4*)&part[wave][t][lane & 15][q * 4] = acc[t];
     __syncthreads();
     const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_scale), leader));
     for (int i = threadIdx.x; i < RT * 256; i += 1024) {
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
       if (tile + t >= tiles || !(its >> at & 1)) continue;
       float sum = 0.f;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) sum += sh.part[v][t][at][rank];
+      for (int v = 0; v < kWaves; ++v) sum += part[v][t][at][rank];
       bf16_t* out = h + (((size_t)(r0 + at) * bank.rank_tiles + tile + t) * 4) * 16 + rank;
       split3(scale * sum, out[0], out[16], out[32]);
       out[48] = (bf16_t)0.f;
@@ -151,38 +155,41 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
   }
 }
 
-// 16 rows and 16 CT columns a wave.  The products of one adapter and rank tile are a step; D steps are asked for at once.
+// 16 rows, 16 CT columns a wave and four times as many a workgroup.  The products of one adapter and rank tile are a step; D steps are asked for at
+// once.  Results pass through LDS, so that base and y are read and written along their rows (64 CT columns of one at a time; in the
+// products' own layout they are 64 bytes of each of sixteen rows, a power of two apart).
 template <typename T, int CT, int D>
 __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_t* h, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                                                           const float* base, int splits, T* y) {
+  constexpr int kCols = 64 * CT, kUnits = kCols / 4;      // units: four columns of a row
+  __shared__ __attribute__((aligned(16))) float sh[kRows][kCols + 4];
   const int m = min(*m_dev, m_upper), r0 = blockIdx.y * kRows;
   if (r0 >= m) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), rr = min(r, m - 1);
-  const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT;
-  if (first >= tiles_n) return;
+  const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT, col0 = blockIdx.x * kCols;
   const int own = adapter_of_row(bank, row_adapter, r, m), my_tiles = own >= 0 ? (bank.ranks()[own] + 15) / 16 : 0;
   const bool wide = bank.n % 4 == 0;                      // four columns of a row at once
-  f32x4 sum[CT], out[CT] = {};
+  f32x4 sum[CT];
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int col = (first + c) * 16 + (lane >> 4) * 4;
-    sum[c] = f32x4{};
-    if (!base || col >= bank.n) continue;
-    for (int s = 0; s < splits; ++s) {
-      const float* from = base + ((size_t)s * m_upper + rr) * bank.n + col;
+  for (int j = 0; j < CT; ++j) {
+    const int unit = j * 256 + threadIdx.x, row = r0 + unit / kUnits, col = col0 + unit % kUnits * 4;
+    sum[j] = f32x4{};
+    if (!base || row >= m || col >= bank.n) continue;
+    const float* from = base + (size_t)row * bank.n + col;
+    for (int s = 0; s < splits; ++s, from += (size_t)m_upper * bank.n) {
       if (wide) {
-        sum[c] += *(const f32x4_unaligned*)from;
+        sum[j] += *(const f32x4_unaligned*)from;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (col + e < bank.n) sum[c][e] += from[e];
+          if (col + e < bank.n) sum[j][e] += from[e];
       }
     }
   }
   const bf16_t* hr = h + (size_t)rr * bank.rank_tiles * 64 + (lane >> 4) * 8;
-  uint64_t todo = __ballot(own >= 0) & 0xffff;
-  int a = -1, t = 0, tiles = 0;                           // the step that comes next; of a row's own adapter the numbers count, whatever h holds otherwise
-  f32x4 acc[CT] = {};
+  uint64_t todo = first < tiles_n ? __ballot(own >= 0) & 0xffff : 0;
+  int a = -1, t = 0, tiles = 0;                           // the step that comes next
+  f32x4 acc[CT] = {}, out[CT] = {};
   auto next = [&]() {
     if (++t < tiles) return;
     t = 0;
@@ -198,7 +205,7 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
   };
   next();
   while (a >= 0) {
-    bf16x8 hi[D], lo[D], w[D][CT];
+    bf16x8 hi[D], lo[D], w[D][CT];                        // (rows of other adapters hold whatever they hold: their results are not taken)
     int step_a[D];
     bool starts[D];
 #pragma unroll
@@ -225,13 +232,16 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
       }
     }
   }
-  if (r >= m) return;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int col = (first + c) * 16 + (lane >> 4) * 4;
-    T* to = y + (size_t)r * bank.n + col;
-    const f32x4 v = own >= 0 ? sum[c] + out[c] : sum[c];
-    if (wide && col < bank.n) {
+  for (int c = 0; c < CT; ++c) *(f32x4*)&sh[lane & 15][(wave * CT + c) * 16 + (lane >> 4) * 4] = out[c];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < CT; ++j) {
+    const int unit = j * 256 + threadIdx.x, row = r0 + unit / kUnits, col = col0 + unit % kUnits * 4;
+    if (row >= m || col >= bank.n) continue;
+    const f32x4 v = sum[j] + *(const f32x4*)&sh[unit / kUnits][unit % kUnits * 4];
+    T* to = y + (size_t)row * bank.n + col;
+    if (wide) {
       if constexpr (sizeof(T) == 2) {
         bf16x4_unaligned b;
 #pragma unroll
@@ -282,20 +292,32 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
   const int tiles = bank.rank_tiles, groups = sl_cdiv(m_upper, kRows);
 #define DOWN_RUN(RT, P)                                                                                                            \
   do {                                                                                                                             \
+    static unsigned long long done = 0;                                                                                            \
+    constexpr int lds = (2 * P > RT ? 2 * P : RT) * 16384;                                                                              \
+    SL_ALLOW_DYNAMIC_LDS(done, (adapters_down_kernel<RT, P>), lds);                                                                  \
     const int z = sl_cdiv(tiles, RT), side = max(2, min(16, 1024 / (groups * z)));                                                   \
-    hipLaunchKernelGGL((adapters_down_kernel<RT, P>), dim3(groups, min(side, m_upper), z), dim3(1024), 0, s, bank, (const bf16_t*)x,    \
+    hipLaunchKernelGGL((adapters_down_kernel<RT, P>), dim3(groups, min(side, m_upper), z), dim3(1024), lds, s, bank, (const bf16_t*)x,  \
                        row_adapter, m_dev, m_upper, h);                                                                              \
   } while (0)
-  if (tiles >= 4 && groups * sl_cdiv(tiles, 4) >= 192) DOWN_RUN(4, 2);
-  else if (tiles >= 2 && groups * sl_cdiv(tiles, 2) >= 192) DOWN_RUN(2, 4);
-  else DOWN_RUN(1, 4);
+  if (tiles >= 4 && groups * sl_cdiv(tiles, 4) >= 128) DOWN_RUN(4, 2);
+  else if (tiles >= 2 && groups * sl_cdiv(tiles, 2) >= 128) DOWN_RUN(2, 2);
+  else DOWN_RUN(1, 2);
 #undef DOWN_RUN
   SL_LAUNCH_CHECK();
-#define UP_RUN(T, CT, D, Y) \
-  hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256), 0, s, bank, h, row_adapter, m_dev, m_upper, \
-                     base, splits, Y)
-  if (y_f32) UP_RUN(float, 2, 4, y_f32);
-  else UP_RUN(bf16_t, 2, 4, (bf16_t*)y_bf16);
+  // columns a wave: more of them share the reading of h and of the rows' adapters, once there are waves enough
+#define UP_RUN(T, CT, D, Y)                                                                                                         \
+  hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256), 0, s, bank, h, row_adapter, m_dev, \
+                     m_upper, base, splits, Y)
+#define UP_BY_SIZE(T, Y)                                                     \
+  do {                                                                       \
+    const int64_t waves = (int64_t)sl_cdiv(ad->n, 16) * groups;              \
+    if (waves < 2048) UP_RUN(T, 1, 4, Y);                                    \
+    else if (waves < 8192) UP_RUN(T, 2, 4, Y);                               \
+    else UP_RUN(T, 4, 2, Y);                                                 \
+  } while (0)
+  if (y_f32) UP_BY_SIZE(float, y_f32);
+  else UP_BY_SIZE(bf16_t, (bf16_t*)y_bf16);
+#undef UP_BY_SIZE
 #undef UP_RUN
   SL_LAUNCH_CHECK();
   return SL_OK;
