@@ -65,10 +65,19 @@ __global__ __launch_bounds__(256) void adapters_pack_kernel(Bank bank, int slot,
   }
 }
 
-// Of the 16 rows from r0 on (lane l: row r0 + l % 16): the lane's adapter, -1 where there is none
-__device__ inline int adapter_of_row(const Bank& bank, const int32_t* row_adapter, int r, int m) {
-  const int a = r < m ? row_adapter[r] : -1;
-  return a >= 0 && a < bank.n_slots && bank.ranks()[a] > 0 ? a : -1;
+// The lane's row's adapter, -1 where there is none, its rank tiles and scale.  (The id is asked for without waiting for the row count.)
+struct Adapter {
+  int id, tiles;
+  float scale;
+};
+__device__ inline Adapter adapter_of_row(const Bank& bank, const int32_t* row_adapter, int r, int m_upper, const int32_t* m_dev, int& m) {
+  int a = row_adapter[min(r, m_upper - 1)];
+  m = min(*m_dev, m_upper);
+  const bool there = r < m && a >= 0 && a < bank.n_slots;
+  a = there ? a : 0;
+  const int tiles = (bank.ranks()[a] + 15) / 16;
+  const float scale = bank.scales()[a];
+  return there && tiles > 0 ? Adapter{a, tiles, scale} : Adapter{-1, 0, 0.f};
 }
 
 // The three parts of v, of 8 bits each
@@ -89,18 +98,18 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
   constexpr int kWaves = 16, kChunk = 512, kChunkBytes = kRows * kChunk * 2;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];      // rows [2][P][16][512], and after them part [kWaves][RT][row][rank]
   auto part = reinterpret_cast<float(*)[RT][16][16]>(lds);
-  const int m = min(*m_dev, m_upper), r0 = blockIdx.x * kRows;
+  const int r0 = blockIdx.x * kRows, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
+  int m;
+  const Adapter mine = adapter_of_row(bank, row_adapter, r0 + (lane & 15), m_upper, m_dev, m);
   if (r0 >= m) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), q = lane >> 4;
-  const int own = adapter_of_row(bank, row_adapter, r, m), my_tiles = own >= 0 ? (bank.ranks()[own] + 15) / 16 : 0;
-  const float my_scale = own >= 0 ? bank.scales()[own] : 0.f;
+  const int own = mine.id;
   const int tile = blockIdx.z * RT, blocks = (bank.k + 31) / 32, chunks = (bank.k + kChunk - 1) / kChunk;
   const bf16_t* xr = x + (size_t)min(r0 + wave, m - 1) * bank.k + lane * 8;
   unsigned char* put = lds + wave * 1024 + (lane ^ wave) * 16;
   const unsigned char* get = lds + (lane & 15) * 1024 + ((wave * 4 + q) ^ (lane & 15)) * 16;
   uint64_t todo = __ballot(own >= 0) & 0xffff;
   for (int place = 0; todo; ++place) {
-    const int leader = __builtin_ctzll(todo), a = __builtin_amdgcn_readlane(own, leader), tiles = __builtin_amdgcn_readlane(my_tiles, leader);
+    const int leader = __builtin_ctzll(todo), a = __builtin_amdgcn_readlane(own, leader), tiles = __builtin_amdgcn_readlane(mine.tiles, leader);
     const uint64_t its = __ballot(own == a);
     todo &= ~its;
     if (place % gridDim.y != blockIdx.y || tile >= tiles) continue;
@@ -140,7 +149,7 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
 #pragma unroll
     for (int t = 0; t < RT; ++t) *(f32x4*)&part[wave][t][lane & 15][q * 4] = acc[t];
     __syncthreads();
-    const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_scale), leader));
+    const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine.scale), leader));
     for (int i = threadIdx.x; i < RT * 256; i += 1024) {
       const int t = i / 256, at = i / 16 % 16, rank = i % 16;
       if (tile + t >= tiles || !(its >> at & 1)) continue;
@@ -156,18 +165,19 @@ __global__ __launch_bounds__(1024) void adapters_down_kernel(Bank bank, const bf
 }
 
 // 16 rows, 16 CT columns a wave and four times as many a workgroup.  The products of one adapter and rank tile are a step; D steps are asked for at
-// once.  Results pass through LDS, so that base and y are read and written along their rows (64 CT columns of one at a time; in the
+// once, while the D before them are worked on.  Results pass through LDS, so that base and y are read and written along their rows (64 CT columns of one at a time; in the
 // products' own layout they are 64 bytes of each of sixteen rows, a power of two apart).
 template <typename T, int CT, int D>
 __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_t* h, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                                                           const float* base, int splits, T* y) {
   constexpr int kCols = 64 * CT, kUnits = kCols / 4;      // units: four columns of a row
-  __shared__ __attribute__((aligned(16))) float sh[kRows][kCols + 4];
-  const int m = min(*m_dev, m_upper), r0 = blockIdx.y * kRows;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];      // h of the 16 rows, and after the products their results
+  auto sh = reinterpret_cast<float(*)[kCols + 4]>(lds);
+  const int r0 = blockIdx.y * kRows, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15);
+  int m;
+  const Adapter mine = adapter_of_row(bank, row_adapter, r, m_upper, m_dev, m);
   if (r0 >= m) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = r0 + (lane & 15), rr = min(r, m - 1);
-  const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT, col0 = blockIdx.x * kCols;
-  const int own = adapter_of_row(bank, row_adapter, r, m), my_tiles = own >= 0 ? (bank.ranks()[own] + 15) / 16 : 0;
+  const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT, col0 = blockIdx.x * kCols, own = mine.id, rr = min(r, m - 1);
   const bool wide = bank.n % 4 == 0;                      // four columns of a row at once
   f32x4 sum[CT];
 #pragma unroll
@@ -186,7 +196,12 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
       }
     }
   }
-  const bf16_t* hr = h + (size_t)rr * bank.rank_tiles * 64 + (lane >> 4) * 8;
+  // (rows of h lie behind one another, in LDS 16 bytes further apart; those of rows without an adapter hold whatever they hold: nothing is taken of them)
+  const int row_pieces = bank.rank_tiles * 8;
+  for (int i = threadIdx.x; i < min(kRows, m - r0) * row_pieces; i += 256)
+    *(uint4*)(lds + (i / row_pieces * (row_pieces + 1) + i % row_pieces) * 16) = *(const uint4*)(h + (size_t)r0 * row_pieces * 8 + i * 8);
+  __syncthreads();
+  const bf16x8* hr = (const bf16x8*)lds + (rr - r0) * (row_pieces + 1) + (lane >> 4);
   uint64_t todo = first < tiles_n ? __ballot(own >= 0) & 0xffff : 0;
   int a = -1, t = 0, tiles = 0;                           // the step that comes next
   f32x4 acc[CT] = {}, out[CT] = {};
@@ -196,7 +211,7 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
     if (todo) {
       const int row = __builtin_ctzll(todo);
       a = __builtin_amdgcn_readlane(own, row);
-      tiles = __builtin_amdgcn_readlane(my_tiles, row);
+      tiles = __builtin_amdgcn_readlane(mine.tiles, row);
       todo &= ~__ballot(own == a);
     } else {
       a = -1;
@@ -204,34 +219,45 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
     }
   };
   next();
-  while (a >= 0) {
-    bf16x8 hi[D], lo[D], w[D][CT];                        // (rows of other adapters hold whatever they hold: their results are not taken)
-    int step_a[D];
-    bool starts[D];
+  struct Steps {
+    bf16x8 w[D][CT];
+    int a[D], t[D];
+  };
+  auto ask = [&](Steps& s) __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      step_a[d] = a;
-      starts[d] = t == 0;
+      s.a[d] = a;
+      s.t[d] = t;
       if (a < 0) continue;
-      hi[d] = *(const bf16x8*)(hr + t * 64);
-      lo[d] = *(const bf16x8*)(hr + t * 64 + 32);
 #pragma unroll
       for (int c = 0; c < CT; ++c)
-        w[d][c] = *((const bf16x8*)bank.b_of(a) + ((size_t)min(first + c, tiles_n - 1) * tiles + t) * 32 + (lane & 31));
+        s.w[d][c] = *((const bf16x8*)bank.b_of(a) + ((size_t)min(first + c, tiles_n - 1) * tiles + t) * 32 + (lane & 31));
       next();
     }
+  };
+  auto work = [&](const Steps& s) __attribute__((always_inline)) {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      if (step_a[d] < 0) break;
+      if (s.a[d] < 0) break;
+      const bf16x8 hi = hr[s.t[d] * 8], lo = hr[s.t[d] * 8 + 4];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
         const f32x4 zero = {};
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[d][c], lo[d], starts[d] ? zero : acc[c], 0, 0, 0);
-        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[d][c], hi[d], acc[c], 0, 0, 0);
-        if (own == step_a[d]) out[c] = acc[c];
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s.w[d][c], lo, s.t[d] == 0 ? zero : acc[c], 0, 0, 0);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(s.w[d][c], hi, acc[c], 0, 0, 0);
+        if (own == s.a[d]) out[c] = acc[c];
       }
     }
+  };
+  Steps even, odd;
+  ask(even);
+  while (even.a[0] >= 0) {
+    ask(odd);
+    work(even);
+    ask(even);
+    work(odd);
   }
+  __syncthreads();
 #pragma unroll
   for (int c = 0; c < CT; ++c) *(f32x4*)&sh[lane & 15][(wave * CT + c) * 16 + (lane >> 4) * 4] = out[c];
   __syncthreads();
@@ -306,14 +332,14 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
   SL_LAUNCH_CHECK();
   // columns a wave: more of them share the reading of h and of the rows' adapters, once there are waves enough
 #define UP_RUN(T, CT, D, Y)                                                                                                         \
-  hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256), 0, s, bank, h, row_adapter, m_dev, \
-                     m_upper, base, splits, Y)
+  hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256),    \
+                     max(kRows * (tiles * 8 + 1) * 16, kRows * (64 * CT + 4) * 4), s, bank, h, row_adapter, m_dev, m_upper, base, splits, Y)
 #define UP_BY_SIZE(T, Y)                                                     \
   do {                                                                       \
     const int64_t waves = (int64_t)sl_cdiv(ad->n, 16) * groups;              \
     if (waves < 2048) UP_RUN(T, 1, 4, Y);                                    \
     else if (waves < 8192) UP_RUN(T, 2, 4, Y);                               \
-    else UP_RUN(T, 4, 2, Y);                                                 \
+    else UP_RUN(T, 4, 1, Y);                                                 \
   } while (0)
   if (y_f32) UP_BY_SIZE(float, y_f32);
   else UP_BY_SIZE(bf16_t, (bf16_t*)y_bf16);
