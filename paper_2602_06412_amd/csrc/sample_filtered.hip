@@ -20,7 +20,8 @@ namespace {
 
 constexpr int kBins = 6144, kDigits = 2048;
 constexpr int kTiny = 0x3a7f;                             // the largest bf16 below 2^-10: its 15 lower bits
-constexpr int kBelow = 1900;                              // bins that the largest number may be below 0: as far as -28
+constexpr int kMiddle = 2560;                             // the tiny numbers' bin: above it numbers to 2^10, below it to -2^18
+constexpr int kTinyList = 4096;
 constexpr int kMaxParts = 1024;                           // 64 times 16 bytes of 1024 threads: 2^18 fp32 numbers
 constexpr double kUnit = 17592186044416.0;                // 2^44
 
@@ -49,6 +50,7 @@ struct Shared {
   uint64_t sums[16], sums2[16];
   uint32_t numbers[16];
   uint64_t found, found2, tiny;
+  uint32_t tinies;
   uint32_t word;
   int index;
   float most[16];
@@ -344,34 +346,24 @@ __device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs&
   }
 }
 
-// Bins of bf16 numbers, 0 the largest's, monotone in z.  With u = max(0, size - kTiny), sizes being the lower 15 bits, the bin is
-// middle - u for positive numbers and middle + u for negative ones: the tiny numbers of both signs are the middle bin, if that is a bin at all.
-struct Bins {
-  int middle, allowed, n;                                 // bins of all numbers above -infinity; of these, counted ones
-  __device__ explicit Bins(float most) {
-    const int bits = (int)(__float_as_uint(most) >> 16), u = max(0, (bits & 0x7fff) - kTiny);
-    middle = bits >> 15 ? -u : u;
-    allowed = middle + 0x7f80 - kTiny;
-    n = min(kBins, allowed);
-  }
-  __device__ int of(float z) const {
-    const int bits = (int)(__float_as_uint(z) >> 16), u = max(0, (bits & 0x7fff) - kTiny);
-    return bits >> 15 ? middle + u : middle - u;
-  }
-  __device__ float number(int b) const { return __uint_as_float((uint32_t)(b < middle ? kTiny + middle - b : (kTiny + b - middle) | 0x8000) << 16); }
-  // whether each_bin's 16 bits hold: no number comes round to another's bin
-  __device__ bool usable() const { return middle > -kBelow && middle < kBins - 1; }
-  // whether a token falls into the middle bin at all
-  __device__ bool any_tiny() const { return middle >= 0; }
-};
+// Bins of bf16 numbers, in descending order.  With u = max(0, size - kTiny), sizes being the lower 15 bits, the bin is kMiddle - u for positive numbers
+// and kMiddle + u for negative ones: the tiny numbers of both signs are the middle bin.
+constexpr int kAllowed = kMiddle + 0x7f80 - kTiny;        // -infinity's
+__device__ inline int bin_of(float z) {
+  const int bits = (int)(__float_as_uint(z) >> 16), u = max(0, (bits & 0x7fff) - kTiny);
+  return bits >> 15 ? kMiddle + u : kMiddle - u;
+}
+__device__ inline float number_of(int b) {
+  return __uint_as_float((uint32_t)(b < kMiddle ? kTiny + kMiddle - b : (kTiny + b - kMiddle) | 0x8000) << 16);
+}
 
-// f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on, NaNs and -infinity are `most`.  Returns whether one of them is
+// f(e, SIZE times the bin) for the eight numbers of a piece; bins from `most` on, numbers beyond bin 0, NaNs and -infinity are `most`.  Returns whether one of them is
 // tiny.  (Step by step for all four words: each step waits for the one before.)
 template <int SIZE, typename F>
-__device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4& piece, F f) {
-  constexpr unsigned short kScale = SIZE >= 4 ? 4 : 1, kFar = SIZE >= 4 ? kBins + kBelow + 64 : 0x7fff;      // (farther ones as far: 4 (middle + u) stays below 2^16)
+__device__ __forceinline__ bool each_bin(int most, const uint4& piece, F f) {
+  constexpr unsigned short kScale = SIZE >= 4 ? 4 : 1, kFar = SIZE >= 4 ? kBins - kMiddle + 64 : 0x7fff;      // (farther ones as far: 4 (middle + u) stays below 2^16)
   const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
-  const u16x2 limit = u16x2{1, 1} * (unsigned short)(most * kScale), middle = u16x2{1, 1} * (unsigned short)(bins.middle * kScale);
+  const u16x2 limit = u16x2{1, 1} * (unsigned short)(most * kScale), middle = u16x2{1, 1} * (unsigned short)(kMiddle * kScale);
   u16x2 u[4], sign[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) u[i] = __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu);
@@ -395,6 +387,12 @@ __device__ __forceinline__ bool each_bin(const Bins& bins, int most, const uint4
     f(2 * i + 1, (b >> 16) * (SIZE / kScale));
   }
   return least[0] == 0 || least[1] == 0;
+}
+
+// The largest bits of a piece's numbers, in two parts: of positive bf16 numbers their bits are in their order, and any negative one's are below.
+__device__ __forceinline__ s16x2 largest_of(const uint4& p) {
+  const auto two = [](uint32_t w) { return __builtin_bit_cast(s16x2, w); };
+  return __builtin_elementwise_max(__builtin_elementwise_max(two(p.x), two(p.y)), __builtin_elementwise_max(two(p.z), two(p.w)));
 }
 
 // f(e) for the tiny numbers of a piece
@@ -425,26 +423,54 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   const int k = a.top_k ? a.top_k[r] : 0;
   if (tid < 256) sh.powers[tid] = exp2(tid / 256.0);
 
+  // the first of the order alone
+  const bool one = !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f;
+  const bool by_count = k > 0 && k < a.vocab && !one, by_mass = p < 1.f && !one, count = sizeof(T) == 2 && (by_count || by_mass);
   float most = -__builtin_inff();
-  const bool unfiltered = a.kept && !(k > 0 && k < a.vocab) && !(p < 1.f) && !(least > 0.f);      // then all tokens are kept: how many?
-  uint32_t number = 0;
-  row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < Row<T, NT>::kVec; ++e) most = fmaxf(most, Row<T, NT>::number(piece, e));
-    if (unfiltered) {
-#pragma unroll
-      for (int e = 0; e < Row<T, NT>::kVec; ++e) number += __popcll(__ballot(allowed(Row<T, NT>::number(piece, e))));
-    }
-  });
-  most = wave_max(most);
-  if (lane == 0) {
-    sh.most[wave] = most;
-    sh.numbers[wave] = number;
+  auto tiny_list = reinterpret_cast<unsigned short*>(sh.part.sum);
+  if (count) {
+    for (int i = tid; i < kBins / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) sh.tiny = sh.tinies = 0;
+    __syncthreads();
+    s16x2 top = {-0x8000, -0x8000};                       // the largest positive number's bits
+    row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
+      const bool small = each_bin<4>(kBins + lane, piece, [&](int, uint32_t at) __attribute__((always_inline)) {
+        atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(sh.counts) + at), 1u);
+      });
+      top = __builtin_elementwise_max(top, largest_of(piece));
+      if (small) each_tiny(piece, [&](int e) __attribute__((always_inline)) {
+        const uint32_t i = atomicAdd(&sh.tinies, 1u);
+        if (i < kTinyList) tiny_list[i] = (unsigned short)(__float_as_uint(Row<T, NT>::number(piece, e)) >> 16);
+      });
+    });
+    most = wave_max((float)max(top[0], top[1]));
+    if (lane == 0) sh.most[wave] = most;
+    __syncthreads();
+    const int bits = (int)wave_max(lane < kWaves ? sh.most[lane] : -__builtin_inff());
+    most = bits > kTiny && bits <= kTiny + kMiddle ? __uint_as_float((uint32_t)bits << 16) : -__builtin_inff();
+    __syncthreads();
   }
-  __syncthreads();
-  most = wave_max(lane < kWaves ? sh.most[lane] : -__builtin_inff());
+  const bool unfiltered = a.kept && !(k > 0 && k < a.vocab) && !(p < 1.f) && !(least > 0.f);      // then all tokens are kept: how many?
   int kept = -1;
-  if (unfiltered) kept = __builtin_amdgcn_readlane(wave_scan32(lane < kWaves ? sh.numbers[lane] : 0), 63);
+  if (!allowed(most)) {
+    uint32_t number = 0;
+    row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < Row<T, NT>::kVec; ++e) most = fmaxf(most, Row<T, NT>::number(piece, e));
+      if (unfiltered) {
+#pragma unroll
+        for (int e = 0; e < Row<T, NT>::kVec; ++e) number += __popcll(__ballot(allowed(Row<T, NT>::number(piece, e))));
+      }
+    });
+    most = wave_max(most);
+    if (lane == 0) {
+      sh.most[wave] = most;
+      sh.numbers[wave] = number;
+    }
+    __syncthreads();
+    most = wave_max(lane < kWaves ? sh.most[lane] : -__builtin_inff());
+    if (unfiltered) kept = __builtin_amdgcn_readlane(wave_scan32(lane < kWaves ? sh.numbers[lane] : 0), 63);
+  }
   if (!allowed(most)) {
     if (tid == 0) {
       a.token[r] = 0;
@@ -453,90 +479,75 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     }
     return;
   }
-  // the first of the order alone
-  const bool one = !(heat > 0.f) || k == 1 || p <= 0.f || least > 1.f;
   if (one) kept = 1;
-  const bool by_count = k > 0 && k < a.vocab && !one, by_mass = p < 1.f && !one;
   const double enough = least > 0.f && !one ? (double)least * kUnit : 0.0;
   const Weigher weight{(double)most, 369.32993046757463 / (double)heat, sh.powers};
 
   if constexpr (sizeof(T) == 2) {
-    const Bins bins(most);
-    int border = bins.allowed;                            // kept: bins below the border, and of the border's tokens the first `need`
+    const int first_bin = bin_of(most);
+    int border = kAllowed;                                // kept: bins below the border, and of the border's tokens the first `need`
     uint32_t need = 0;
     uint64_t each = 0;
-    // whether the bins do: a finite maximum, and no weight beyond them
-    bool counted = !one && most < __builtin_inff() && bins.usable() && (bins.n == bins.allowed || weight(bins.number(kBins - 1)) == 0);
-    if (one) {
-      // the bins of the largest and of everything else
-      if (bins.middle != 0 && bins.usable()) {
-        counted = true;
-        border = 0;
-        need = 1;
-        each = (uint64_t)kUnit;
-      }
+    // whether the bins do: they hold the largest number, and there is no weight beyond them
+    bool counted = !one && most < __builtin_inff() && first_bin >= 0 && first_bin < kBins && weight(number_of(kBins - 1)) == 0 && (!count || sh.tinies <= kTinyList);
+    if (one && first_bin >= 0 && first_bin < kBins && first_bin != kMiddle) {
+      counted = true;
+      border = first_bin;
+      need = 1;
+      each = (uint64_t)kUnit;
     }
-    if (counted && (by_count || by_mass)) {
-      for (int i = tid; i < kBins / 4; i += NT) reinterpret_cast<uint4*>(sh.counts)[i] = make_uint4(0, 0, 0, 0);
-      if (tid == 0) sh.tiny = 0;
-      __syncthreads();
-      row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
-        const bool small = each_bin<4>(bins, kBins + lane, piece, [&](int, uint32_t at) __attribute__((always_inline)) {
-          atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<unsigned char*>(sh.counts) + at), 1u);
-        });
-        if (small) each_tiny(piece, [&](int e) __attribute__((always_inline)) { atomicAdd((unsigned long long*)&sh.tiny, (unsigned long long)weight(Row<T, NT>::number(piece, e))); });
-      });
+    if (counted && count) {
+      for (uint32_t i = tid; i < sh.tinies; i += NT)
+        atomicAdd((unsigned long long*)&sh.tiny, (unsigned long long)weight(__uint_as_float((uint32_t)tiny_list[i] << 16)));
       __syncthreads();
       // neighbouring bins a thread
       constexpr int kMine = kBins / NT;
       const uint64_t tiny = sh.tiny;
       uint64_t mass = 0, total;
-      uint32_t n[kMine], count = 0, all;
+      uint32_t n[kMine], number = 0, all;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int b = tid * kMine + i;
         n[i] = sh.counts[b];
-        n[i] = b < bins.n ? n[i] : 0;
-        count += n[i];
+        number += n[i];
       }
-      if (__any(count > 0)) {
+      if (__any(number > 0)) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
           const int b = tid * kMine + i;
-          const uint64_t w = n[i] * weight(bins.number(b));
-          mass += b == bins.middle ? tiny : w;
+          const uint64_t w = n[i] * weight(number_of(b));
+          mass += b == kMiddle ? tiny : w;
         }
       }
       const uint64_t my_mass = mass;
-      const uint32_t my_count = count;
-      before_me2<NT>(mass, count, sh, total, all);
+      const uint32_t my_number = number;
+      before_me2<NT>(mass, number, sh, total, all);
 #pragma unroll 1
       for (int round = 0; round < 2; ++round) {
         if (!(round ? by_mass : by_count)) continue;
-        if (!round && (uint32_t)k > all) {                // all tokens, if there are no more than those counted
-          counted = bins.n == bins.allowed;
-          if (!counted) break;
-          continue;
+        if (!round && (uint32_t)k > all) {                // (whether more tokens lie beyond the bins is not known)
+          counted = false;
+          break;
         }
         const double goal = round ? (double)p * (double)total : (double)k;
-        const double before = round ? (double)mass : (double)count, up_to = round ? (double)(mass + my_mass) : (double)(count + my_count);
+        const double before = round ? (double)mass : (double)number, up_to = round ? (double)(mass + my_mass) : (double)(number + my_number);
         if (before < goal && goal <= up_to) {
           sh.index = tid;
           sh.found = mass;
-          sh.word = count;
+          sh.word = number;
         }
         __syncthreads();
         // every wave finds the number on its own
         const int b = sh.index * kMine + lane;
-        const uint32_t n = lane >= kMine ? 0 : b == border ? need : b < min(border, bins.n) ? sh.counts[b] : 0;
-        const uint64_t w = n && b != bins.middle ? weight(bins.number(b)) : 0, here = n == 0 ? 0 : b == bins.middle ? tiny : n * w;
+        const uint32_t n = lane >= kMine ? 0 : b == border ? need : b < min(border, kBins) ? sh.counts[b] : 0;
+        const uint64_t w = n && b != kMiddle ? weight(number_of(b)) : 0, here = n == 0 ? 0 : b == kMiddle ? tiny : n * w;
         const uint64_t masses = sh.found + wave_scan(here);
         const uint32_t counts = sh.word + wave_scan32(n);
         const int first = __builtin_ctzll(__ballot((round ? (double)masses : (double)counts) >= goal || lane == kMine - 1));
         const uint32_t n_there = __builtin_amdgcn_readlane(n, first), n_before = __builtin_amdgcn_readlane(counts - n, first);
         const uint64_t m_before = lane_of(masses - here, first);
         border = sh.index * kMine + first;
-        if (border == bins.middle) {
+        if (border == kMiddle) {
           counted = false;
           break;
         }
@@ -549,12 +560,12 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     }
     if (counted && enough > 0) {
       // the first bin whose weight is not enough: near where the logarithm says
-      const int b = bins.of((float)((double)most + (double)heat * log((double)least))) - 31 + lane;
+      const int b = bin_of((float)((double)most + (double)heat * log((double)least))) - 31 + lane;
       const float tiny_most = 0x1.fep-11f;                 // the largest bf16 below 2^-10
       const bool tiny_first = (double)weight(fminf(most, tiny_most)) >= enough, tiny_last = (double)weight(-tiny_most) >= enough;
-      const bool passes = b < 0 || (b < bins.n && (b == bins.middle ? tiny_last : (double)weight(bins.number(b)) >= enough));
+      const bool passes = b <= first_bin || (b < kBins && (b == kMiddle ? tiny_last : (double)weight(number_of(b)) >= enough));
       const uint64_t passing = __ballot(passes);
-      if (!(passing & 1) || passing >> 63 || (bins.any_tiny() && tiny_first != tiny_last)) {
+      if (!(passing & 1) || passing >> 63 || (most > -tiny_most && tiny_first != tiny_last)) {
         counted = false;
       } else {
         const int limit = lane_of((uint64_t)(uint32_t)b, 0) + __builtin_ctzll(~passing);
@@ -567,25 +578,24 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     }
     if (counted) {
       // weights of the bins that are kept, as far as they are not 0 (exp(-31.2) 2^44 is below 1/2); a 0 for the border and one for all others
-      const int table = max(0, min(min(border, bins.n), bins.of((float)((double)most - 31.2 * (double)heat)) + 2));
+      const int table = one ? border : min(min(border, kBins), bin_of((float)((double)most - 31.2 * (double)heat)) + 2);
       __syncthreads();
-      for (int b = tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != bins.middle ? weight(bins.number(b)) : 0;
+      for (int b = first_bin + tid; b <= table + 1; b += NT) sh.weights[b] = b < table && b != kMiddle ? weight(number_of(b)) : 0;
       __syncthreads();
       const uint32_t on_border = need > 0 && border == table ? border * 8 : 0xffff;      // (tokens of a border further down weigh nothing)
       // where what is kept is positive, a wave looks at its largest number first (positive bf16 numbers are in the order of their bits)
-      const int lowest = table < bins.middle ? (int)(__float_as_uint(bins.number(table)) >> 16) : -0x8000;
+      const int lowest = table < kMiddle ? (int)(__float_as_uint(number_of(table)) >> 16) : -0x8000;
       draw(row, sh, a, r, need, each, kept, [&](const uint4& p) __attribute__((always_inline)) {
-        const auto two = [](uint32_t w) { return __builtin_bit_cast(s16x2, w); };
-        const s16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(p.x), two(p.y)), __builtin_elementwise_max(two(p.z), two(p.w)));
+        const s16x2 m = largest_of(p);
         return (bool)__any(max(m[0], m[1]) >= lowest);
       }, [&](const uint4& piece, auto f, auto g) __attribute__((always_inline)) {
-        const bool small = each_bin<8>(bins, table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
+        const bool small = each_bin<8>(table + 1, piece, [&](int e, uint32_t at) __attribute__((always_inline)) {
           f(e, at == on_border, *reinterpret_cast<const uint64_t*>(reinterpret_cast<const unsigned char*>(sh.weights) + at));
         });
-        if (small && bins.middle < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
+        if (small && kMiddle < table) each_tiny(piece, [&](int e) __attribute__((always_inline)) { g(e, weight(Row<T, NT>::number(piece, e))); });
       }, [&](const uint4& piece) __attribute__((always_inline)) {
         uint32_t n = 0;
-        each_bin<1>(bins, bins.allowed, piece, [&](int, uint32_t b) __attribute__((always_inline)) { n += (int)b < border; });
+        each_bin<1>(kAllowed, piece, [&](int, uint32_t b) __attribute__((always_inline)) { n += (int)b < border; });
         return n;
       });
       return;
@@ -593,6 +603,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   }
 
   // the border's key digit by digit: by count, then by mass
+  __syncthreads();
   if (!one && !unfiltered) kept = -1;
   constexpr int kSlow = sizeof(T) == 2 ? 1 : 4;           // (of bf16 rows few come here)
   uint32_t border = one ? key_of(most) : 0x007fffffu;     // (-infinity's)
