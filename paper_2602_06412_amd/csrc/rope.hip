@@ -37,31 +37,84 @@ __device__ inline float2 turn_of(double pos, double f, float amplitude) {
   return make_float2((float)((q == 1 || q == 2 ? -cq : cq) * amplitude), (float)((q >= 2 ? -sq : sq) * amplitude));
 }
 
-// A workgroup turns one row; a thread takes pairs, and single numbers behind them.
-template <typename TI, typename TO, bool PAIRS>
+// V numbers that lie together, as fp32
+template <int V, typename T>
+__device__ inline void load_v(const T* p, float (&v)[V]) {
+  if constexpr (V == 1) {
+    v[0] = st<T>::ld(p);
+  } else if constexpr (V == 8) {
+    ld8(p, v);
+  } else if constexpr (sizeof(T) == 2) {
+    const bf16x4_t u = *reinterpret_cast<const bf16x4_t*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)u[e];
+  } else {
+    ld4f(p, v);
+  }
+}
+template <int V, typename T>
+__device__ inline void store_v(T* p, const float (&v)[V]) {
+  if constexpr (V == 1) st<T>::stv(p, v[0]);
+  else if constexpr (V == 8) st8(p, v);
+  else if constexpr (sizeof(T) == 2) st4(p, v);
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// A workgroup turns one row; a thread takes V pairs at a time, and V single numbers behind them.  The turns of a row are formed once, for all of its
+// heads.
+template <typename TI, typename TO, bool PAIRS, int V>
 __global__ __launch_bounds__(kThreads) void rope_rows_kernel(RopeArgs a) {
-  __shared__ float2 turn[kMaxRot / 2];
+  __shared__ __attribute__((aligned(16))) float cosine[kMaxRot / 2], sine[kMaxRot / 2];
   const int r = blockIdx.x;
   if (r >= min(*a.m_dev, a.m_upper)) return;
   const double pos = a.row_pos[r];
   const int half = a.rot / 2, rest = a.d - a.rot;
-  for (int j = threadIdx.x; j < half; j += kThreads) turn[j] = turn_of(pos, a.freqs[j], a.amplitude);
+  for (int j = threadIdx.x; j < half; j += kThreads) {
+    const float2 t = turn_of(pos, a.freqs[j], a.amplitude);
+    cosine[j] = t.x;
+    sine[j] = t.y;
+  }
   __syncthreads();
+  const int n = half / V, n_rest = rest / V;
   for (int w = 0; w < 2; ++w) {
     const RopeSide& x = a.side[w];
     const TI* in = (const TI*)x.in + (size_t)r * x.in_stride;
     TO* out = (TO*)x.out + (size_t)r * x.out_stride;
-    for (int i = threadIdx.x; i < x.heads * half; i += kThreads) {
-      const int h = i / half, j = i - h * half, at = h * a.d + (PAIRS ? 2 * j : j), with = at + (PAIRS ? 1 : half);
-      const float u = st<TI>::ld(in + at), v = st<TI>::ld(in + with);
-      const float2 t = turn[j];
-      st<TO>::stv(out + at, u * t.x - v * t.y);
-      st<TO>::stv(out + with, u * t.y + v * t.x);
+    for (int i = threadIdx.x; i < x.heads * n; i += kThreads) {
+      const int h = i / n, j = (i - h * n) * V, at = h * a.d + (PAIRS ? 2 * j : j), with = at + (PAIRS ? V : half);
+      float u[V], v[V], p[V], q[V];
+      load_v<V>(in + at, u);
+      load_v<V>(in + with, v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        // of neighbours in pairs the first V numbers are half of the pairs, the second V the other half
+        constexpr int kHalf = V / 2;
+        const float c = cosine[j + e], s = sine[j + e];
+        const float f = !PAIRS || V == 1 ? u[e] : e < kHalf ? u[2 * e % V] : v[2 * e % V], g = !PAIRS || V == 1 ? v[e] : e < kHalf ? u[(2 * e + 1) % V] : v[(2 * e + 1) % V];
+        p[e] = f * c - g * s;
+        q[e] = f * s + g * c;
+      }
+      if constexpr (PAIRS && V > 1) {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+          u[2 * e] = p[e];
+          u[2 * e + 1] = q[e];
+          v[2 * e] = p[V / 2 + e];
+          v[2 * e + 1] = q[V / 2 + e];
+        }
+        store_v<V>(out + at, u);
+        store_v<V>(out + with, v);
+      } else {
+        store_v<V>(out + at, p);
+        store_v<V>(out + with, q);
+      }
     }
     if ((const void*)in == (const void*)out) continue;
-    for (int i = threadIdx.x; i < x.heads * rest; i += kThreads) {
-      const int h = i / rest, at = h * a.d + a.rot + i - h * rest;
-      st<TO>::stv(out + at, st<TI>::ld(in + at));
+    for (int i = threadIdx.x; i < x.heads * n_rest; i += kThreads) {
+      const int h = i / n_rest, at = h * a.d + a.rot + (i - h * n_rest) * V;
+      float u[V];
+      load_v<V>(in + at, u);
+      store_v<V>(out + at, u);
     }
   }
 }
@@ -95,16 +148,35 @@ int slk_rope_rows(hipStream_t s, const void* q, int64_t q_stride, void* q_out, i
                   float amplitude, const int32_t* row_pos, const int32_t* m_dev, int m_upper) {
   const RopeArgs a{{{q, q_out, q_stride, q_out_stride, n_heads}, {k, k_out, k_stride, k_out_stride, k ? n_kv_heads : 0}},
                    freqs, row_pos, m_dev, m_upper, d, rot, amplitude};
-#define ROPE_RUN(TI, TO)                                                                                                      \
-  do {                                                                                                                        \
-    if (pairs) hipLaunchKernelGGL((rope_rows_kernel<TI, TO, true>), dim3(m_upper), dim3(kThreads), 0, s, a);                  \
-    else hipLaunchKernelGGL((rope_rows_kernel<TI, TO, false>), dim3(m_upper), dim3(kThreads), 0, s, a);                       \
+  // numbers at a time: eight of bf16, four where one side is fp32, if every piece of them is aligned
+  const int most = dtype_in == SL_BF16 && dtype_out == SL_BF16 ? 8 : 4;
+  auto fits = [&](int v) {
+    auto side = [&](const RopeSide& x) {
+      return ((uintptr_t)x.in % (v * sl_tsize(dtype_in)) | (uintptr_t)x.out % (v * sl_tsize(dtype_out))) == 0 && x.in_stride % v == 0 && x.out_stride % v == 0;
+    };
+    return rot / 2 % v == 0 && (d - rot) % v == 0 && d % v == 0 && side(a.side[0]) && (!k || side(a.side[1]));
+  };
+  const int v = fits(most) ? most : fits(4) ? 4 : 1;
+#define ROPE_LAUNCH(TI, TO, PAIRS, V) hipLaunchKernelGGL((rope_rows_kernel<TI, TO, PAIRS, V>), dim3(m_upper), dim3(kThreads), 0, s, a)
+#define ROPE_BY_LAYOUT(TI, TO, V)                                                             \
+  do {                                                                                        \
+    if (pairs) ROPE_LAUNCH(TI, TO, true, V); else ROPE_LAUNCH(TI, TO, false, V);                \
+  } while (0)
+#define ROPE_RUN(TI, TO)                                                                      \
+  do {                                                                                        \
+    if (v == 1) ROPE_BY_LAYOUT(TI, TO, 1); else ROPE_BY_LAYOUT(TI, TO, 4);                      \
   } while (0)
   if (dtype_in == SL_BF16) {
-    if (dtype_out == SL_BF16) ROPE_RUN(bf16_t, bf16_t); else ROPE_RUN(bf16_t, float);
+    if (dtype_out == SL_BF16) {
+      if (v == 8) ROPE_BY_LAYOUT(bf16_t, bf16_t, 8); else ROPE_RUN(bf16_t, bf16_t);
+    } else {
+      ROPE_RUN(bf16_t, float);
+    }
   } else {
     if (dtype_out == SL_BF16) ROPE_RUN(float, bf16_t); else ROPE_RUN(float, float);
   }
+#undef ROPE_BY_LAYOUT
+#undef ROPE_LAUNCH
 #undef ROPE_RUN
   SL_LAUNCH_CHECK();
   return SL_OK;
