@@ -73,6 +73,17 @@ def test_forward(m, m_upper, n, k, slots, max_rank, splits, run, out):
     check(y[:m], x[:m], base[:, :m] if base is not None else None, which[:m], weights) if weights else None
 
 
+# the other forms that sizes choose: more rank tiles a workgroup, more columns a wave
+LARGE = [(520, 520, 1041, 72, 6, 256, 1, 9), (700, 703, 801, 136, 5, 80, 0, 11), (1030, 1030, 528, 520, 4, 80, 2, 40), (513, 515, 4099, 264, 7, 16, 1, 50), (520, 520, 4100, 136, 3, 40, 1, 33),
+         (2040, 2050, 20, 24, 2, 64, 1, 100), (2040, 2050, 1040, 8, 2, 32, 0, 1)]
+
+
+@pytest.mark.parametrize("m,m_upper,n,k,slots,max_rank,splits,run", LARGE)
+@pytest.mark.parametrize("out", [F, BF])
+def test_forward_of_many_rows(m, m_upper, n, k, slots, max_rank, splits, run, out):
+    test_forward(m, m_upper, n, k, slots, max_rank, splits, run, out)
+
+
 @pytest.mark.parametrize("ids", [[-5, 2 ** 31 - 1, 3, -2 ** 31], [1, 1, 1, 1], [0, 1, 0, 1], [2, 2, 2, 0]])
 def test_ids_that_name_no_adapter_get_the_base_alone(ids):
     ad, weights = bank(3, 16, 72, 64, {0: 16, 1: 5}, 1)          # slot 2 is empty

@@ -207,3 +207,87 @@ def test_same_results_captured_and_on_another_stream(m, vocab):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[2])
+
+
+ALL_FILTERS = dict(top_k=[0, 40, 0, 300, 0], top_p=[0.9, 1.0, 0.5, 0.95, 1.0], min_p=[0.0, 0.0, 0.02, 0.001, 0.0], temperature=[1.0, 0.8, 1.3])
+
+
+def all_filters(m):
+    return {n: np.resize(np.array(v, np.float64), m) for n, v in ALL_FILTERS.items()}
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("m,vocab", [(256, 900), (257, 900), (300, 4104), (257, 1 << 18), (258, 126463)])
+def test_many_rows(m, vocab, dtype):
+    """More rows than CUs: smaller workgroups.  Of four rows of logits, each drawn from again and again; the first twenty against the definition."""
+    z = bell(4, vocab, dtype, m)
+    u = np.resize(np.random.default_rng(m).random(20).astype(np.float32), m)
+    filters, to = all_filters(m), np.resize([2, 0, 3, 1], m)
+    got = draw(z, u, row_map=to, **filters)
+    check(z, u[:20], [g[:20] for g in got], row_map=to, **{n: v[:20] for n, v in filters.items()})
+    seen = {}
+    for r in range(m):
+        key = (u[r], to[r]) + tuple(v[r] for v in filters.values())
+        assert seen.setdefault(key, [g[r] for g in got]) == [g[r] for g in got]
+
+
+def spans(vocab, seed):
+    """Rows of bf16 numbers in places of their own: by name, what they hold."""
+    g = torch.Generator().manual_seed(seed)
+    n = torch.randn(vocab, generator=g)
+    some = torch.rand(vocab, generator=g) < 0.5
+    return {
+        "large": n * 500 + 3000, "large and small": torch.where(some, n, n * 300 + 900), "negative": n * 2 - 14, "far below": torch.where(some, n, torch.tensor(-3e5)),
+        "far below too": torch.where(some, n, torch.tensor(torch.finfo(BF).min)), "tiny": n * 2.0 ** -13, "tiny and below": torch.where(some, n * 2.0 ** -13, -n.abs() - 1),
+        "tiny and above": torch.where(some, n * 2.0 ** -13, n.abs() * 2), "subnormal": n * 1e-39, "zeros": torch.where(some, torch.tensor(0.0), torch.tensor(-0.0)), "at the tiny ones' end":
+        torch.where(some, torch.tensor(2.0 ** -10), torch.tensor(2.0 ** -10 - 2.0 ** -18)) * torch.sign(n), "steps of 2^-7": torch.round(n * 128) / 128, "negative and tiny": torch.where(some, -n.abs() * 2.0 ** -13, -n.abs() - 0.01),
+        "wide": n * 200, "one far above": torch.where(torch.arange(vocab) == vocab // 3, torch.tensor(1e30), n),
+    }
+
+
+SPANS = list(spans(2, 0))
+
+
+@pytest.mark.parametrize("name", SPANS)
+@pytest.mark.parametrize("vocab", [60, 5001, 20000])
+def test_numbers_of_every_size(name, vocab):
+    """Where numbers lie decides how a bf16 row is worked on: one by one or digit by digit.  (At 20000 there are more tiny numbers than are listed.)"""
+    kinds = [{}, dict(top_k=3), dict(top_k=vocab // 3), dict(top_k=vocab - 1), dict(top_k=vocab * 3 // 4, top_p=0.7), dict(top_p=0.3), dict(top_p=0.9999), dict(min_p=0.3), dict(min_p=0.9995),
+             dict(top_p=0.8, temperature=1e4), dict(min_p=0.5, temperature=1e5), dict(top_k=vocab // 2, top_p=0.9, min_p=0.05, temperature=30.0), dict(temperature=0.0),
+             dict(top_p=0.9, min_p=0.9999, temperature=2.0 ** -12), dict(top_k=vocab // 2, min_p=1e-30), dict(top_k=1)]
+    plain = dict(top_k=0, top_p=1.0, min_p=0.0, temperature=1.0)
+    filters = {n: np.array([k.get(n, v) for k in kinds]) for n, v in plain.items()}
+    z = spans(vocab, vocab)[name].to(BF).repeat(len(kinds), 1).to(DEV)
+    u = np.random.default_rng(vocab + SPANS.index(name)).random(len(kinds)).astype(np.float32)
+    check(z, u, draw(z, u, **filters), **filters)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_rows_far_apart(dtype):
+    """Offsets beyond 2^31 numbers: rows 2^20 numbers apart, the last of them 2^31 and more from the first."""
+    n = (1 << 11) + 3
+    store = torch.empty((n - 1 << 20) + 1000, dtype=dtype, device=DEV)
+    z = store.as_strided((n, 1000), (1 << 20, 1))
+    rows = [0, 1, n - 3, n - 1]
+    z[rows] = bell(4, 1000, dtype, 8)
+    u = np.random.default_rng(9).random(4).astype(np.float32)
+    filters = all_filters(4)
+    got = draw(z, u, row_map=rows, **filters)
+    check(z[rows], u, got, **filters)
+
+
+def test_two_draws_at_once_and_twice():
+    """Two streams with a workspace each, many times: the same tokens every time."""
+    m, vocab = 40, 9000
+    z = bell(m, vocab, BF, 11)
+    u, m_dev, p = dev(np.random.default_rng(12).random(m), F), dev([m], torch.int32), dev(np.full(m, 0.9), F)
+    ws = [torch.empty(max(256, B.sl_sample_filtered_bytes(m, vocab)), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs = torch.full((2, 20, m), -1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(20):
+        for w, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                B.sl_sample_filtered(z, m_dev, m, u, outs[w, i], ws[w], top_p=p)
+    torch.cuda.synchronize()
+    assert bool((outs == outs[0, 0]).all()) and int(outs.min()) >= 0
