@@ -8,7 +8,9 @@
 //              given up also clears the entry that it came from, so that no two lanes touch one entry
 //   returns    a page given up and not taken: onto the stack, and its entry cleared
 //   copies     (states apart) all other entries of the table and of the stack
-// Every workgroup forms the prefix sums again from the lengths, a wave for all 255 sequences: no second launch, no atomics.
+// Every workgroup forms the prefix sums again from the lengths, a wave for all 255 sequences, lanes moved instead of LDS: no second launch, no
+// atomics.  What bounds it is the chain of loads and sums of that wave and one search in them, not bytes.  Replayed from a graph: 3 sequences
+// 4.2 us (3 us are a launch's own), 255 sequences that decode 5.4 us, 64 sequences with prompts of 100000 slots, not all of which fit, 7.6 us.
 #include "sl_common.h"
 
 namespace {
@@ -45,94 +47,73 @@ __device__ inline int owner(const int* start, int i) {
   return b;
 }
 
-__device__ inline int64_t wave_sum64(int64_t v) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor((long long)v, o, 64);
-  return v;
-}
-
 // By one wave, four sequences a lane.
 __device__ void make_plan(const PagesArgs& a, Plan& p) {
   const int lane = threadIdx.x & 63, shift = a.page_shift;
   const int64_t most = (int64_t)a.max_pages << shift;      // <= 2^30
   const int free_pages = min(max(*a.n_free, 0), a.n_pages);
-  int old_len[4], want[4], gone[4], need[4];
-  int64_t gone_all = 0, need_all = 0, more_all = 0;
-  bool over = false;
+  int old_len[4], want[4], gone[4], need[4], more[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int b = lane * 4 + i;
     const bool there = b < a.batch;
     old_len[i] = there ? (int)min((int64_t)max(a.seq_len[b], 0), most) : 0;
     want[i] = there ? a.want[b] : 0;
-    if (want[i] < 0) want[i] = old_len[i];
+    if (want[i] < 0 || want[i] > most) want[i] = old_len[i];
     const int change = pages_of(want[i], shift) - pages_of(old_len[i], shift);
     gone[i] = max(-change, 0);
     need[i] = max(change, 0);
-    gone_all += gone[i];
-    need_all += need[i];
-    more_all += max(want[i] - old_len[i], 0);
-    over |= want[i] > most;
+    more[i] = max(want[i] - old_len[i], 0);
   }
-  gone_all = wave_sum64(gone_all);
-  need_all = wave_sum64(need_all);
-  more_all = wave_sum64(more_all);
-  if (__any(over) || need_all > free_pages + gone_all || more_all > a.m_upper) {
-    // not room for all: one after another
+  // sequences that there is no room for stay.  Those before the first of them are served; what they leave is too little for it, and for
+  // others behind it: these stay too, and the rest is looked at again.
+  const uint32_t gone_to_me = wave_scan32(gone[0] + gone[1] + gone[2] + gone[3]);
+  const int64_t left = (int64_t)free_pages + (uint32_t)__builtin_amdgcn_readlane(gone_to_me, 63);
+  while (true) {
+    const int64_t needs = (int64_t)need[0] + need[1] + need[2] + need[3], mores = (int64_t)more[0] + more[1] + more[2] + more[3];
+    int64_t n = (int64_t)wave_scan(needs) - needs, m = (int64_t)wave_scan(mores) - mores, n_left = 0, m_left = 0;      // left for the first without room
+    int first = 4;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      p.old_len[lane * 4 + i] = old_len[i];
-      p.new_len[lane * 4 + i] = want[i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (lane == 0) {
-      int64_t left = free_pages + gone_all, room = a.m_upper;
-      for (int b = 0; b < a.batch; ++b) {
-        const int o = p.old_len[b], w = p.new_len[b];
-        if (w <= o) continue;
-        const int n = pages_of(w, shift) - pages_of(o, shift);
-        if (w > most || n > left || w - o > room) {
-          p.new_len[b] = o;
-        } else {
-          left -= n;
-          room -= w - o;
-        }
+      if (first == 4 && (n + need[i] > left || m + more[i] > a.m_upper)) {
+        first = i;
+        n_left = left - n;
+        m_left = a.m_upper - m;
       }
+      n += need[i];
+      m += more[i];
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    const uint64_t without = __ballot(first < 4);
+    if (!without) break;
+    const int where = __builtin_ctzll(without), first_seq = where * 4 + __builtin_amdgcn_readlane(first, where);
+    n_left = (int64_t)lane_of(n_left, where);
+    m_left = (int64_t)lane_of(m_left, where);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      want[i] = p.new_len[lane * 4 + i];
-      need[i] = max(pages_of(want[i], shift) - pages_of(old_len[i], shift), 0);
+      if (lane * 4 + i < first_seq || (need[i] <= n_left && more[i] <= m_left)) continue;
+      want[i] -= more[i];
+      need[i] = more[i] = 0;
     }
   }
-  int v[4][4];                                            // [what][sequence]: given up, taken, rows, pieces
+  uint32_t v[4][4];                                       // [what][sequence]: given up, taken, rows, pieces
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool grows = want[i] > old_len[i];
     v[0][i] = gone[i];
     v[1][i] = need[i];
-    v[2][i] = grows ? want[i] - old_len[i] : 0;
-    v[3][i] = grows ? pages_of(want[i], shift) - (old_len[i] >> shift) : 0;
+    v[2][i] = more[i];
+    v[3][i] = more[i] ? pages_of(want[i], shift) - (old_len[i] >> shift) : 0;
   }
   int* const to[4] = {p.gone, p.taken, p.rows, p.pieces};
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const int own = v[w][0] + v[w][1] + v[w][2] + v[w][3];
-    int sum = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int below = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += below;
-    }
-    int at = sum - own;
+    const uint32_t own = v[w][0] + v[w][1] + v[w][2] + v[w][3], sum = w ? wave_scan32(own) : gone_to_me;
+    uint32_t at = sum - own;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      to[w][lane * 4 + i] = at;
+      to[w][lane * 4 + i] = (int)at;
       at += v[w][i];
     }
-    if (lane == 63) to[w][kSeqs] = at;
+    if (lane == 63) to[w][kSeqs] = (int)sum;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -203,8 +184,8 @@ __global__ __launch_bounds__(kThreads) void kv8_pages_kernel(PagesArgs a) {
     a.to.table[source] = -1;
   }
   if (!a.apart) return;
-  for (int64_t i = start; i < (int64_t)a.batch * a.max_pages; i += step) {
-    const int b = (int)(i / a.max_pages), j = (int)(i - (int64_t)b * a.max_pages);
+  for (int i = start; i < a.batch * a.max_pages; i += step) {      // (<= 2^30)
+    const int b = i / a.max_pages, j = i - b * a.max_pages;
     const int had = pages_of(p.old_len[b], shift), has = pages_of(p.new_len[b], shift);
     if (j < min(had, has) || j >= max(had, has)) a.to.table[i] = a.from.table[i];
   }
@@ -226,7 +207,9 @@ __global__ __launch_bounds__(kThreads) void kv8_pages_init_kernel(Pages to, int 
   if (start == 0) *to.n_free = n_pages;
 }
 
-unsigned grid_for(int64_t numbers) { return (unsigned)max((int64_t)1, min((int64_t)512, (numbers + 2047) / 2048)); }
+// One number a thread: workgroups that take 2048 each are too few (255 sequences that decode 10.3 us, 512 each 7.1, 256 each 6.2; of as
+// few as 128 nothing is gained).  More than 512 workgroups form the sums oftener than they save (2048 of them: 16.9 us for 15.7).
+unsigned grid_for(int64_t numbers) { return (unsigned)max((int64_t)1, min((int64_t)512, (numbers + 255) / 256)); }
 
 }  // namespace
 

@@ -83,36 +83,6 @@ struct Weigher {
   }
 };
 
-// ---- sums over lanes, by moving lanes ----
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-template <int CTRL, int ROWS>
-__device__ inline uint64_t moved(uint64_t v) {
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 15, true), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 15, true);
-  return __builtin_bit_cast(uint64_t, u32x2{lo, hi});
-}
-// of this lane and those before it
-__device__ inline uint64_t wave_scan(uint64_t v) {
-  v += moved<0x111, 15>(v);                               // within 16 lanes, from 1, 2, 4 and 8 below
-  v += moved<0x112, 15>(v);
-  v += moved<0x114, 15>(v);
-  v += moved<0x118, 15>(v);
-  v += moved<0x142, 10>(v);                               // the first and third sixteen's last lane to the one behind
-  v += moved<0x143, 12>(v);                               // lane 31 to the upper half
-  return v;
-}
-__device__ inline uint32_t wave_scan32(uint32_t v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 15, 15, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 15, 15, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 15, 15, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 15, 15, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 10, 15, true);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 12, 15, true);
-  return v;
-}
-__device__ inline uint64_t lane_of(uint64_t v, int lane) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-}
-
 // sum over the block of the threads before this one; `whole` gets the sum of all
 template <int NT>
 __device__ inline uint64_t before_me(uint64_t v, Shared& sh, uint64_t& whole) {

@@ -115,6 +115,34 @@ __device__ inline float wave_max(float v) {
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
 }
+// Sums over this lane and those before it, of whole numbers, by moving lanes (all 64 have to be there)
+__device__ inline uint32_t wave_scan32(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 15, 15, true);      // within 16 lanes, from 1, 2, 4 and 8 below
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 15, 15, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 10, 15, true);      // the first and third sixteen's last lane to the one behind
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 12, 15, true);      // lane 31 to the upper half
+  return v;
+}
+template <int CTRL, int ROWS>
+__device__ inline uint64_t moved_lanes(uint64_t v) {
+  typedef uint32_t pair __attribute__((ext_vector_type(2)));
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, CTRL, ROWS, 15, true), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), CTRL, ROWS, 15, true);
+  return __builtin_bit_cast(uint64_t, pair{lo, hi});
+}
+__device__ inline uint64_t wave_scan(uint64_t v) {
+  v += moved_lanes<0x111, 15>(v);
+  v += moved_lanes<0x112, 15>(v);
+  v += moved_lanes<0x114, 15>(v);
+  v += moved_lanes<0x118, 15>(v);
+  v += moved_lanes<0x142, 10>(v);
+  v += moved_lanes<0x143, 12>(v);
+  return v;
+}
+__device__ inline uint64_t lane_of(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
 // Sum over a block of NT threads; every thread gets the result.  `sh` has NT/64 floats.
 template <int NT>
 __device__ inline float block_sum(float v, float* sh) {

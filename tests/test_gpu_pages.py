@@ -93,6 +93,22 @@ def test_one_that_does_not_fit_does_not_keep_others_out():
     assert pages.seq_len.tolist() == [17, 0, 30] and got["cu"] == [0, 1, 1, 1]
 
 
+@pytest.mark.parametrize("spare,m_upper", [(500, 1 << 20), (20000, 3000), (300, 2000), (0, 500), (37, 37)])
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_little_room_for_growth_of_every_size(spare, m_upper, seed):
+    """Who is served depends on all before: growth from one slot to far more than there is room for."""
+    rng = random.Random(seed)
+    page, batch, max_pages = 16, 255, 210
+    lens = [rng.randint(0, 40) for _ in range(batch)]
+    table, stack, n_free = pool(rng, lens, page, max_pages, spare)
+    want = [rng.choice([n + int(2 ** rng.uniform(0, 11.7)), n // 2, n + 1]) for n in lens]
+    pages = B.KV8Pages(len(stack), page, batch, max_pages)
+    state(pages, table, lens, stack, n_free)
+    expected = ref.pages_resize(table, lens, stack, n_free, want, page, len(stack), m_upper)
+    assert any(n < w for n, w in zip(expected[1], want))
+    check(pages, resize(pages, want, m_upper), expected)
+
+
 def test_longer_than_a_sequence_can_be_and_lengths_out_of_range():
     pages = B.KV8Pages(20, 16, 4, 2)
     for want in ([33, 32, 2 ** 31 - 1, 1], [-2 ** 31, 32, -5, 40]):
