@@ -600,8 +600,8 @@ int sl_adapters_pack(void *stream, const sl_adapters *ad /* host */, int32_t slo
  *   workspace    sl_adapters_workspace_bytes bytes, 256-byte aligned; needs no initialisation, calls that may overlap in time must not
  *                share one
  * Rows past the count are neither read nor written, and no row touches another's result.  Products are accumulated in fp32; A x[r] is held in
- * fp32 and goes into the second product with 24 bits; a result is rounded once.  An A x[r] whose product with scale leaves fp32's range
- * comes out as NaN or an infinity.  The same sums in the same order in every call of one shape.  m_upper <= 2^16. */
+ * fp32 and goes into the second product with 24 bits; a result is rounded once.  A row with an adapter whose x holds a NaN or an infinity,
+ * or whose scale A x[r] leaves the range of bf16 (3.4e38), comes out as NaN.  The same sums in the same order in every call of one shape.  m_upper <= 2^16. */
 int sl_adapters_workspace_bytes(const sl_adapters *ad /* host */, int32_t m_upper, size_t *out);
 int sl_adapters_forward(void *stream, const sl_adapters *ad /* host */, const void *x, const int32_t *row_adapter, const int32_t *m_dev,
                         int32_t m_upper, const float *base, int32_t splits, float *y_f32, void *y_bf16, void *workspace,
@@ -622,8 +622,8 @@ int sl_adapters_forward(void *stream, const sl_adapters *ad /* host */, const vo
  *   temperature f32, top_k i32, top_p f32, min_p f32: [m_upper] each, or null: 1, and no filter
  *   uniform  [m_upper] f32 in [0, 1); taken as the nearest number there, NaN as 0
  *   token    [m_upper] i32 out; prob [m_upper] f32 out or null: W of the token over the sum of kept W; kept [m_upper] i32 out or null: their number
- *   workspace  sl_sample_filtered_bytes bytes, 256-byte aligned; needs no initialisation, calls that may overlap in time must not
- *            share one
+ *   workspace  sl_sample_filtered_bytes bytes, 256-byte aligned; needs no initialisation (nothing is kept there at present: all sums
+ *            stay on the CU), calls that may overlap in time must not share one
  * A row without a token to draw gets token 0, prob 0 and kept 0.  Rows past min(*m_dev, m_upper) are neither read nor written; m_upper <= 2^20. */
 int sl_sample_filtered_bytes(int32_t m_upper, int32_t vocab, size_t *out);
 int sl_sample_filtered(void *stream, const void *logits, int32_t dtype, int64_t row_stride, int32_t n_rows, int32_t vocab,

@@ -12,6 +12,10 @@
 //                                                      product takes the same numbers again, for another part of h
 // Ranks, inputs and outputs past the matrices are zeros.
 // h between the launches: [row][rank tiles][high, middle, low part, zeros][16]
+//
+// What bounds it: one row, two short launches (7.8 us replayed); 64 rows of 64 adapters of rank 16, 4096 to 12288, 17.6 us, the
+// adapters' 134 MB being 7.6 TB/s of it; 1100 rows in runs of one adapter of rank 64, 12288 to 4096, beside two partial sums, 38 us for
+// 76 MB, of which the first product's passing of x through LDS is the longer half.
 #include "sl_common.h"
 
 namespace {
@@ -313,8 +317,10 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
                          const float* base, int splits, float* y_f32, void* y_bf16, void* workspace) {
   const Bank bank = bank_of(ad);
   bf16_t* h = (bf16_t*)workspace;
-  // rank tiles a workgroup: as many as leave one for each CU (each reads the rows again); adapters of sixteen rows side by side: all of them
-  // while that is no more than a few workgroups for each CU
+  // Rank tiles a workgroup: as many as leave a workgroup for every second CU (each reads the rows again).  1100 rows of rank 64, the whole call with
+  // 1 / 2 / 4 tiles: 52.3 / 43.5 / 46.9 us.  Adapters of sixteen rows side by side: all of them while that is no more than four workgroups a
+  // CU, and two at least.  One / by this rule / sixteen: 16 rows of 16 adapters 52 / 13.1 / 13.1 us, 512 rows of 64 63 / 23.8 / 23.9, 2048 rows
+  // of 64 90 / 62.4 / 68.3, 2048 rows in runs of 200 23.5 / 21.3 / 24.4.
   const int tiles = bank.rank_tiles, groups = sl_cdiv(m_upper, kRows);
 #define DOWN_RUN(RT, P)                                                                                                            \
   do {                                                                                                                             \
@@ -330,7 +336,9 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
   else DOWN_RUN(1, 2);
 #undef DOWN_RUN
   SL_LAUNCH_CHECK();
-  // columns a wave: more of them share the reading of h and of the rows' adapters, once there are waves enough
+  // Column tiles a wave: more of them share the reading of h and of the rows' adapters, once there are waves enough.  The whole call with 1 / 2 /
+  // 4: 64 rows by 4096 of rank 64 (1024 waves of one tile) 27.2 / 33.3 / - us, 64 rows by 12288 (3,000) 23.6 / 21.0 / 21.4, 256 rows by 12288
+  // (12,000) - / 18.8 / 16.5, 2048 rows by 4096 (33,000) - / 25.8 / 24.7.
 #define UP_RUN(T, CT, D, Y)                                                                                                         \
   hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256),    \
                      max(kRows * (tiles * 8 + 1) * 16, kRows * (64 * CT + 4) * 4), s, bank, h, row_adapter, m_dev, m_upper, base, splits, Y)

@@ -4,6 +4,9 @@
 // turns of pos f fall away exactly in fp64 (and what the product's rounding left, as much as 2^-26 of a turn at the largest positions, is
 // added again), what is left is taken to within an eighth of a turn by exact steps of a quarter, and there the Taylor sums of sine and
 // cosine, through the 11th and 12th power (the next terms are below 1e-11), are rounded to fp32 once.
+//
+// What bounds it is reading and writing the rows: 5533 rows of 32 + 32 heads of 128 bf16 take 36 us, which is the rate of a large copy (4.9 TB/s);
+// 137 rows of fp32, half of each head turned, 8 us where the caller marshals each call, and 3 us replayed from a graph, a launch's own.
 #include "sl_common.h"
 
 namespace {
@@ -148,7 +151,8 @@ int slk_rope_rows(hipStream_t s, const void* q, int64_t q_stride, void* q_out, i
                   float amplitude, const int32_t* row_pos, const int32_t* m_dev, int m_upper) {
   const RopeArgs a{{{q, q_out, q_stride, q_out_stride, n_heads}, {k, k_out, k_stride, k_out_stride, k ? n_kv_heads : 0}},
                    freqs, row_pos, m_dev, m_upper, d, rot, amplitude};
-  // numbers at a time: eight of bf16, four where one side is fp32, if every piece of them is aligned
+  // numbers at a time: eight of bf16, four where one side is fp32, if every piece of them is aligned.  40 heads of 128 bf16, replayed, 8 / 4 / 1 at
+  // a time: 512 rows 3.8 / 4.0 / 5.2 us, 8192 rows 26.0 / 26.0 / 31.1; 5533 rows of 64 heads 36 us of eight, 49 of one
   const int most = dtype_in == SL_BF16 && dtype_out == SL_BF16 ? 8 : 4;
   auto fits = [&](int v) {
     auto side = [&](const RopeSide& x) {

@@ -4,7 +4,11 @@
 // and, in order of ids, some of those that equal it.  Weights are whole numbers, W = rint(2^44 exp((z - max) / T)): at most 2^18 of them
 // add up to less than 2^63, in any order and from any thread, to the same sum.
 //
-// A workgroup takes a row and passes over it as often as it has to, 32 to 64 bytes a thread in flight.
+// A workgroup takes a row and passes over it as often as it has to, 32 to 64 bytes a thread in flight.  Of bf16 that is twice (counts, with the
+// largest number; then weights in order of ids), and what bounds it is those reads and an LDS access a token: 1024 rows of 126464, top-p and min-p, 113 us,
+// 4.6 TB/s over both passes (one read of all rows at the rate of a large one: 38 us); 64 rows, top-k and top-p, 36 us, each
+// on a CU of its own, whose share of the passes is 11 GB/s times 1000 and the rest the search for two borders.  Several workgroups a row, in three launches, were slower
+// for top-k (27 -> 30 us), for many rows and for short ones, and gained a tenth in the best case: one workgroup it is.
 //
 // Weights.  2^t = 2^n T[i] 2^(r / 256) with 256 t = 256 n + i + r, |r| <= 1 / 2: a table of 256 powers and a sum of four terms, off by
 // less than 2^-51 of itself.
@@ -13,7 +17,9 @@
 // taken once for each number that occurs; the last pass reads the weights of what is kept from a table.  Numbers below 2^-10 in size, nearly
 // half of the 65536 and hardly any logit, share one bin and are weighed token by token.
 // fp32, and bf16 where that does not do (a border among the tiny numbers, a temperature in the hundreds): the border's key in three
-// steps of 11, 11 and 10 bits, each a pass that adds up weights (or counts) for each value of the digit.
+// steps of 11, 11 and 10 bits that add up weights (or counts) for each value of the digit.  The first is a pass over the row; the second lists the
+// keys that begin with the first's digit, in LDS, and it and the third work on the list (if that has no room for all, on the row).  What bounds
+// it is the fp64 of a weight for each token and pass: 64 rows of 126464 fp32, top-p, 116 us (130 with three passes over the row), top-k 68 (76), no filter 49.
 #include "sl_common.h"
 
 namespace {
@@ -21,7 +27,8 @@ namespace {
 constexpr int kBins = 6144, kDigits = 2048;
 constexpr int kTiny = 0x3a7f;                             // the largest bf16 below 2^-10: its 15 lower bits
 constexpr int kMiddle = 2560;                             // the tiny numbers' bin: above it numbers to 2^10, below it to -2^18
-constexpr int kTinyList = 4096;
+constexpr int kTinyList = 4096;                           // (16-bit numbers, where the parts' sums come later)
+constexpr int kList = 8192;
 constexpr int kMaxParts = 1024;                           // 64 times 16 bytes of 1024 threads: 2^18 fp32 numbers
 constexpr double kUnit = 17592186044416.0;                // 2^44
 
@@ -40,7 +47,10 @@ struct Shared {
   union {
     uint32_t counts[kBins + 64];                          // (the last: what is beyond the bins, a place for each lane)
     uint64_t weights[kBins + 2];
-    uint64_t digits[kDigits];
+    struct {
+      uint64_t digits[kDigits];
+      uint32_t list[kList];                               // keys that begin with the border's first digit
+    };
   };
   struct {                                                // of a wave's part of a piece, in order of ids
     uint64_t sum[kMaxParts];
@@ -50,12 +60,13 @@ struct Shared {
   uint64_t sums[16], sums2[16];
   uint32_t numbers[16];
   uint64_t found, found2, tiny;
-  uint32_t tinies;
+  uint32_t tinies, listed;
   uint32_t word;
   int index;
   float most[16];
 };
 static_assert(sizeof(Shared) <= 64 * 1024, "two workgroups a CU");
+static_assert(kTinyList * 2 <= sizeof(Shared::part.sum), "the list of tiny numbers");
 
 // fp32 as a number whose order is that of z (both zeros alike)
 __device__ inline uint32_t key_of(float z) {
@@ -588,17 +599,42 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     uint32_t prefix = 0;
     uint64_t above = 0;
     int shift = 32;
+    bool listed = false;
 #pragma unroll 1
     for (int step = 0; step < 3; ++step) {
       const int bits = step < 2 ? 11 : 10, upper = shift;
       shift -= bits;
       for (int i = tid; i < kDigits; i += NT) sh.digits[i] = 0;
+      if (tid == 0 && step == 0) sh.listed = 0;
       __syncthreads();
-      row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
-        const uint32_t key = key_of(z);
-        if (inside(key, z) && (step == 0 || key >> upper == prefix))
-          atomicAdd((unsigned long long*)&sh.digits[key >> shift & ((1 << bits) - 1)], (unsigned long long)(round ? weight(z) : 1));
-      });
+      auto add = [&](uint32_t key, float z) __attribute__((always_inline)) {
+        atomicAdd((unsigned long long*)&sh.digits[key >> shift & ((1 << bits) - 1)], (unsigned long long)(round ? weight(z) : 1));
+      };
+      if (step == 1) {
+        row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
+          const uint32_t key = key_of(z);
+          const bool in = inside(key, z) && key >> upper == prefix;
+          const uint64_t all = __ballot(in);
+          if (!all) return;
+          int at = 0;
+          if (lane == 0) at = (int)atomicAdd(&sh.listed, (uint32_t)__popcll(all));
+          at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+          if (in && at < kList) sh.list[at] = key;
+        });
+        __syncthreads();
+        listed = sh.listed <= kList;
+      }
+      if (listed) {
+        for (uint32_t i = tid; i < sh.listed; i += NT) {
+          const uint32_t key = sh.list[i];
+          if (step == 1 || key >> upper == prefix) add(key, of_key(key));
+        }
+      } else {
+        row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
+          const uint32_t key = key_of(z);
+          if (inside(key, z) && (step == 0 || key >> upper == prefix)) add(key, z);
+        });
+      }
       __syncthreads();
       // neighbouring digits a thread, descending
       constexpr int kMine = kDigits / NT;
@@ -678,7 +714,11 @@ int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t ro
                         const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace) {
   const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
 #define SAMPLE_RUN(T, NT) hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), 0, s, a)
-  const bool many = m_upper > 256;
+  // Rows beyond the CUs: two workgroups of 512 threads a CU pass over more rows at a time, one of 1024 over a row faster.  512 / 1024 threads,
+  // us: 126464 bf16 64 rows 40.4 / 36.4, 256 rows 46.2 / 41.8, 300 rows 59 / 64, 512 rows 64 / 78, 1024 rows 117 / 148; 8192 bf16 256 rows
+  // 12.6 / 13.7, 512 rows 16 / 24; 126464 fp32 256 rows 187 / 150, 300 rows 231 / 176, 384 rows 237 / 235, 512 rows 246 / 251; 8192 fp32
+  // 300 rows 24.9 / 25.3, 384 rows 25 / 33.
+  const bool many = m_upper > (dtype == SL_BF16 ? 256 : 320);
   if (dtype == SL_BF16) {
     if (many) SAMPLE_RUN(bf16_t, 512); else SAMPLE_RUN(bf16_t, 1024);
   } else {

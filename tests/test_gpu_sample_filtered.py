@@ -217,7 +217,7 @@ def all_filters(m):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
-@pytest.mark.parametrize("m,vocab", [(256, 900), (257, 900), (300, 4104), (257, 1 << 18), (258, 126463)])
+@pytest.mark.parametrize("m,vocab", [(256, 900), (257, 900), (300, 4104), (257, 1 << 18), (258, 126463), (321, 1 << 18), (330, 5001)])
 def test_many_rows(m, vocab, dtype):
     """More rows than CUs: smaller workgroups.  Of four rows of logits, each drawn from again and again; the first twenty against the definition."""
     z = bell(4, vocab, dtype, m)
