@@ -135,6 +135,7 @@ struct Row {
   static constexpr int kVec = st<T>::kVec, kSpan = NT * kVec, kThreads = NT, kBits = 128 / kVec;
   const T* z;
   int vocab;
+  uint4 only;                                             // of a row of one piece or less: it
 
   __device__ __forceinline__ int n() const { return (vocab + kSpan - 1) / kSpan; }
   __device__ __forceinline__ uint4 fetch(int c) const {
@@ -189,7 +190,7 @@ struct Row {
       __builtin_amdgcn_sched_barrier(0);                  // (one after another: registers)
     };
     uint4 a[2] = {}, b[2] = {}, last = {};
-    if (full * kSpan < vocab) last = fetch(full);
+    if (full * kSpan < vocab) last = full ? fetch(full) : only;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (i < full) a[i] = whole(i);
@@ -298,7 +299,7 @@ __device__ __forceinline__ void draw(const R& row, Shared& sh, const SampleArgs&
   if (sh.index % kParts != wave) return;
   // the part that holds it, once more
   const int c = sh.index / kParts, id = c * R::kSpan + tid * R::kVec;
-  const uint4 p = row.fetch(c);
+  const uint4 p = row.vocab < R::kSpan ? row.only : row.fetch(c);
   uint64_t w[R::kVec] = {}, mine = 0;
   uint32_t tie[R::kVec] = {}, my_ties = 0;
   weigh(p, [&](int e, bool is_tie, uint64_t v) __attribute__((always_inline)) {
@@ -394,14 +395,15 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   __shared__ __attribute__((aligned(16))) Shared sh;
   constexpr int kWaves = NT / 64;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // (asked for together with the row count)
+  const int at = a.row_map ? a.row_map[r] : r, k = a.top_k ? a.top_k[r] : 0;
+  const float heat = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
   if (r >= min(*a.m_dev, a.m_upper)) return;
-  const int at = a.row_map ? a.row_map[r] : r;
   const bool there = at >= 0 && at < a.n_rows;
   Row<T, NT> row;
   row.z = (const T*)a.logits + (size_t)(there ? at : 0) * a.row_stride;
   row.vocab = there ? a.vocab : 0;
-  const float heat = a.temperature ? a.temperature[r] : 1.f, p = a.top_p ? a.top_p[r] : 1.f, least = a.min_p ? a.min_p[r] : 0.f;
-  const int k = a.top_k ? a.top_k[r] : 0;
+  row.only = row.vocab < Row<T, NT>::kSpan ? row.fetch(0) : uint4{};
   if (tid < 256) sh.powers[tid] = exp2(tid / 256.0);
 
   // the first of the order alone
@@ -717,8 +719,9 @@ int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t ro
   // Rows beyond the CUs: two workgroups of 512 threads a CU pass over more rows at a time, one of 1024 over a row faster.  512 / 1024 threads,
   // us: 126464 bf16 64 rows 40.4 / 36.4, 256 rows 46.2 / 41.8, 300 rows 59 / 64, 512 rows 64 / 78, 1024 rows 117 / 148; 8192 bf16 256 rows
   // 12.6 / 13.7, 512 rows 16 / 24; 126464 fp32 256 rows 187 / 150, 300 rows 231 / 176, 384 rows 237 / 235, 512 rows 246 / 251; 8192 fp32
-  // 300 rows 24.9 / 25.3, 384 rows 25 / 33.
-  const bool many = m_upper > (dtype == SL_BF16 ? 256 : 320);
+  // 300 rows 24.9 / 25.3, 384 rows 25 / 33.  And few rows that are short, of which most is waiting for one another: 3 rows of 1024 bf16 9.6 / 10.7,
+  // 8192 bf16 12.0 / 13.0, 16384 bf16 14.3 / 14.7, 1024 fp32 10.6 / 11.8, 4096 fp32 14.8 / 15.1, 8192 fp32 19.6 / 18.3 (256 threads are slower than 512).
+  const bool many = m_upper > (dtype == SL_BF16 ? 256 : 320) || vocab * sl_tsize(dtype) <= 16384;
   if (dtype == SL_BF16) {
     if (many) SAMPLE_RUN(bf16_t, 512); else SAMPLE_RUN(bf16_t, 1024);
   } else {
