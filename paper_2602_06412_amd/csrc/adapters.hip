@@ -183,23 +183,23 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
   if (r0 >= m) return;
   const int tiles_n = (bank.n + 15) / 16, first = (blockIdx.x * 4 + wave) * CT, col0 = blockIdx.x * kCols, own = mine.id, rr = min(r, m - 1);
   const bool wide = bank.n % 4 == 0;                      // four columns of a row at once
-  f32x4 sum[CT];
-#pragma unroll
-  for (int j = 0; j < CT; ++j) {
+  // base: the first two planes are asked for here and added up behind the products
+  auto plane = [&](int j, int s) __attribute__((always_inline)) {
     const int unit = j * 256 + threadIdx.x, row = r0 + unit / kUnits, col = col0 + unit % kUnits * 4;
-    sum[j] = f32x4{};
-    if (!base || row >= m || col >= bank.n) continue;
-    const float* from = base + (size_t)row * bank.n + col;
-    for (int s = 0; s < splits; ++s, from += (size_t)m_upper * bank.n) {
-      if (wide) {
-        sum[j] += *(const f32x4_unaligned*)from;
-      } else {
+    f32x4 v = {};
+    if (!base || s >= splits || row >= m || col >= bank.n) return v;
+    const float* from = base + ((size_t)s * m_upper + row) * bank.n + col;
+    if (wide) return (f32x4)*(const f32x4_unaligned*)from;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + e < bank.n) sum[j][e] += from[e];
-      }
-    }
-  }
+    for (int e = 0; e < 4; ++e)
+      if (col + e < bank.n) v[e] = from[e];
+    return v;
+  };
+  f32x4 sum[CT], then[CT];
+#pragma unroll
+  for (int j = 0; j < CT; ++j) sum[j] = plane(j, 0);
+#pragma unroll
+  for (int j = 0; j < CT; ++j) then[j] = plane(j, 1);
   // (rows of h lie behind one another, in LDS 16 bytes further apart; those of rows without an adapter hold whatever they hold: nothing is taken of them)
   const int row_pieces = bank.rank_tiles * 8;
   for (int i = threadIdx.x; i < min(kRows, m - r0) * row_pieces; i += 256)
@@ -265,6 +265,13 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
 #pragma unroll
   for (int c = 0; c < CT; ++c) *(f32x4*)&sh[lane & 15][(wave * CT + c) * 16 + (lane >> 4) * 4] = out[c];
   __syncthreads();
+  for (int s = 2;; ++s) {
+#pragma unroll
+    for (int j = 0; j < CT; ++j) sum[j] += then[j];
+    if (s >= splits) break;
+#pragma unroll
+    for (int j = 0; j < CT; ++j) then[j] = plane(j, s);
+  }
 #pragma unroll
   for (int j = 0; j < CT; ++j) {
     const int unit = j * 256 + threadIdx.x, row = r0 + unit / kUnits, col = col0 + unit % kUnits * 4;

@@ -10,7 +10,7 @@
 //   copies     (states apart) all other entries of the table and of the stack
 // Every workgroup forms the prefix sums again from the lengths, a wave for all 255 sequences, lanes moved instead of LDS: no second launch, no
 // atomics.  What bounds it is the chain of loads and sums of that wave and one search in them, not bytes.  Replayed from a graph: 3 sequences
-// 4.2 us (3 us are a launch's own), 255 sequences that decode 5.4 us, 64 sequences with prompts of 100000 slots, not all of which fit, 7.6 us.
+// 4.2 us (3 us are a launch's own), 255 sequences that decode 5.4 us, 64 sequences of which half want 176000 slots more, not all of which fit, 7.6 us.
 #include "sl_common.h"
 
 namespace {
