@@ -533,7 +533,7 @@ int sl_kv8_pages_init(void *stream, const sl_kv8_pages *pages /* host */);
  *   given up (b, then place), the rest from the top of the stack; what is given up and not taken goes on top of the stack.
  *   from, to    the state before and after: the same struct contents (in place), or states that share no buffer but agree in their
  *               sizes; then every entry of `to` is written and `from` stays as it is, so that a step can be taken back
- *   want_len [batch] i32, not the seq_len of `to`
+ *   want_len [batch] i32, not the seq_len of `to`; no output may overlap it or another output
  *   cu_rows  [batch + 1] i32 out: rows cu_rows[b] .. cu_rows[b + 1] - 1 are the new slots of sequence b, ascending
  *   row_pos  [m_upper] i32 out: the row's slot in its sequence
  *   row_len  [m_upper] i32 out or null: row_pos + 1 (what a row sees in causal order)

@@ -14,8 +14,8 @@
 // h between the launches: [row][rank tiles][high, middle, low part, zeros][16]
 //
 // What bounds it: waiting for one load after another (a row's adapter, its rank, h, weights), twice.  One row of 4096, 7.8 us replayed, two
-// launches of 4; 64 rows of 64 adapters of rank 16, 4096 to 12288 beside fp32, 17.6 us (8.3 and 10.2 for 31 MB in all, at the rate of a large read 4.5);
-// 1100 rows in runs of one adapter of rank 64, 12288 to 4096 beside two partial sums, 38 us (20.3 and 18.1 for 83 MB, at that rate 12.2).
+// launches of 4; 64 rows of 64 adapters of rank 16, 4096 to 12288 beside fp32, 17.3 us (8.3 and 9.8 for 31 MB in all, at the rate of a large read 4.5);
+// 1100 rows in runs of one adapter of rank 64, 12288 to 4096 beside two partial sums, 36 us (20.3 and 16 for 83 MB, at that rate 12.2).
 #include "sl_common.h"
 
 namespace {

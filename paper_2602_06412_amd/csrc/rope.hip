@@ -6,7 +6,7 @@
 // cosine, through the 11th and 12th power (the next terms are below 1e-11), are rounded to fp32 once.
 //
 // What bounds it is reading and writing the rows: 5533 rows of 32 + 32 heads of 128 bf16 take 36 us, which is the rate of a large copy (4.9 TB/s);
-// 137 rows of fp32, half of each head turned, 8 us where the caller marshals each call, and 3 us replayed from a graph, a launch's own.
+// 137 rows of fp32, half of each head turned, 8 us where the caller marshals each call, and 4 us replayed from a graph, of which 3 are a launch's own.
 #include "sl_common.h"
 
 namespace {
