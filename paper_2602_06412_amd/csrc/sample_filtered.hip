@@ -19,7 +19,8 @@
 // fp32, and bf16 where that does not do (a border among the tiny numbers, a temperature in the hundreds): the border's key in three
 // steps of 11, 11 and 10 bits that add up weights (or counts) for each value of the digit.  The first is a pass over the row; the second lists the
 // keys that begin with the first's digit, in LDS, and it and the third work on the list (if that has no room for all, on the row).  What bounds
-// it is the fp64 of a weight for each token and pass: 64 rows of 126464 fp32, top-p, 116 us (130 with three passes over the row), top-k 68 (76), no filter 49.
+// it is the fp64 of a weight for each token and pass: 64 rows of 126464 fp32, top-p, 116 us (130 with three passes over the row),
+// top-k 63 (76; 68 with a pass of its own for the first digit), no filter 49.
 #include "sl_common.h"
 
 namespace {
@@ -435,11 +436,24 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
   }
   const bool unfiltered = a.kept && !(k > 0 && k < a.vocab) && !(p < 1.f) && !(least > 0.f);      // then all tokens are kept: how many?
   int kept = -1;
+  // (fp32: the first digit of top-k's border is counted where the maximum is found)
+  const bool early = sizeof(T) == 4 && by_count;
   if (!allowed(most)) {
     uint32_t number = 0;
+    if (early) {
+      for (int i = tid; i < kDigits; i += NT) sh.digits[i] = 0;
+      __syncthreads();
+    }
     row.pieces([&](int, const uint4& piece) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < Row<T, NT>::kVec; ++e) most = fmaxf(most, Row<T, NT>::number(piece, e));
+      if (early) {
+#pragma unroll
+        for (int e = 0; e < Row<T, NT>::kVec; ++e) {
+          const float z = Row<T, NT>::number(piece, e);
+          if (allowed(z)) atomicAdd((unsigned long long*)&sh.digits[key_of(z) >> 21], 1ull);
+        }
+      }
       if (unfiltered) {
 #pragma unroll
         for (int e = 0; e < Row<T, NT>::kVec; ++e) number += __popcll(__ballot(allowed(Row<T, NT>::number(piece, e))));
@@ -606,7 +620,8 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
     for (int step = 0; step < 3; ++step) {
       const int bits = step < 2 ? 11 : 10, upper = shift;
       shift -= bits;
-      for (int i = tid; i < kDigits; i += NT) sh.digits[i] = 0;
+      const bool counted = early && !round && step == 0;
+      for (int i = tid; i < kDigits && !counted; i += NT) sh.digits[i] = 0;
       if (tid == 0 && step == 0) sh.listed = 0;
       __syncthreads();
       auto add = [&](uint32_t key, float z) __attribute__((always_inline)) {
@@ -631,7 +646,7 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
           const uint32_t key = sh.list[i];
           if (step == 1 || key >> upper == prefix) add(key, of_key(key));
         }
-      } else {
+      } else if (!counted) {
         row.template each<kSlow>([&](float z) __attribute__((always_inline)) {
           const uint32_t key = key_of(z);
           if (inside(key, z) && (step == 0 || key >> upper == prefix)) add(key, z);
