@@ -1,9 +1,9 @@
 // Rotary positions of rows of queries and keys, as a call of its own.
 //
 // A pair (a, b) turns by t = 2 pi pos f: (a cos t - b sin t, a sin t + b cos t).  Frequencies are kept in turns per slot, so the whole
-// turns of pos f fall away exactly in fp64 (and what the product's rounding left, as much as 2^-26 of a turn at the largest positions, is
-// added again), what is left is taken to within an eighth of a turn by exact steps of a quarter, and there the Taylor sums of sine and
-// cosine, through the 11th and 12th power (the next terms are below 1e-11), are rounded to fp32 once.
+// turns of pos f fall away in one fused step: the product with all of its bits, of which fp64 alone would lose as much as 2^-25 of a turn at
+// the largest positions, less a whole number, rounded once.  What is left is taken to within an eighth of a turn by exact steps of a quarter, and
+// there the Taylor sums of sine and cosine, through the 11th and 12th power (the next terms are below 1e-11), are rounded to fp32 once.
 //
 // What bounds it is reading and writing the rows: 5533 rows of 32 + 32 heads of 128 bf16 take 36 us, which is the rate of a large copy (4.9 TB/s);
 // 137 rows of fp32, half of each head turned, 8 us where the caller marshals each call, and 4 us replayed from a graph, of which 3 are a launch's own.
@@ -30,7 +30,7 @@ struct RopeArgs {
 
 // amplitude (cos, sin) of 2 pi pos f
 __device__ inline float2 turn_of(double pos, double f, float amplitude) {
-  const double product = pos * f, turns = (product - rint(product)) + fma(pos, f, -product);
+  const double turns = fma(pos, f, -rint(pos * f));
   const double quarter = rint(4.0 * turns);
   const double x = (turns - 0.25 * quarter) * 6.283185307179586476925, y = x * x;      // |x| <= pi / 4
   const double s = x * fma(y, fma(y, fma(y, fma(y, fma(y, -1.0 / 39916800, 1.0 / 362880), -1.0 / 5040), 1.0 / 120), -1.0 / 6), 1.0);

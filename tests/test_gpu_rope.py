@@ -157,3 +157,36 @@ def test_same_bits_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+
+
+def turned_exactly(pos, f):
+    """cos and sin of 2 pi pos f [rows, pairs], right to 2^-52: f is a fraction over a power of two, so whole turns fall away in whole numbers."""
+    turns = np.empty((len(pos), len(f)))
+    for j, x in enumerate(f):
+        above, below = float(x).as_integer_ratio()
+        for i, p in enumerate(pos):
+            left = int(p) * above % below
+            turns[i, j] = (left if 2 * left <= below else left - below) / below
+    return np.cos(2 * np.pi * turns), np.sin(2 * np.pi * turns)
+
+
+@pytest.mark.parametrize("d", [6, 64])                           # one pair at a time, and four
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("t_in", [F, BF])
+def test_sine_and_cosine_are_rounded_once_at_any_position(d, interleaved, t_in):
+    """The pairs (1, 0) and (0, 1) turn into sine and cosine alone: half a step of fp32, and 2^-36 for Taylor's sums, whose next terms are below 7e-12."""
+    rng = np.random.default_rng(d)
+    pos = np.concatenate([[0, 1, -1, 2 ** 31 - 1, -(2 ** 31), 2 ** 28 + 1, -(2 ** 30) - 1], rng.integers(-(2 ** 31), 2 ** 31, 200),
+                          rng.integers(2 ** 31 - 10 ** 6, 2 ** 31, 60), rng.integers(-(2 ** 20), 2 ** 20, 60)])
+    m, half = len(pos), d // 2
+    f = f64(freqs_on_gpu(d))
+    f[-1] = 1000.3                                               # a caller's own
+    first, second = (slice(0, d, 2), slice(1, d, 2)) if interleaved else (slice(0, half), slice(half, d))
+    x = torch.zeros(m, 2, d, dtype=t_in, device=DEV)
+    x[:, 0, first] = x[:, 1, second] = 1
+    y = torch.empty(m, 2, d, device=DEV)
+    B.sl_rope_rows(x, y, None, None, dev(f, torch.float64), dev(pos, torch.int32), dev([m], torch.int32), m, interleaved=interleaved)
+    c, s = turned_exactly(pos, f)
+    y = f64(y)
+    for got, want in ((y[:, 0, first], c), (y[:, 0, second], s), (y[:, 1, first], -s), (y[:, 1, second], c)):
+        assert (np.abs(got - want) <= np.abs(want) * 2.0 ** -24 + 2.0 ** -36).all(), np.abs(got - want).max()
