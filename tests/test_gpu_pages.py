@@ -154,3 +154,48 @@ def test_captured_steps_of_one_state(m_upper):
         torch.cuda.synchronize()
         for x, y in ((a.page_table, e.page_table), (a.seq_len, e.seq_len), (a.n_free, e.n_free), (a.free_pages, e.free_pages), (cu, cu2), (pos, pos2)):
             assert torch.equal(x, y), i
+
+
+def test_many_pages_given_up_in_place_take_no_longer_than_beside():
+    """A step that only releases: a million pages, no rows.  What is done in place is less than what states apart take, by however few rows the call is bounded."""
+    page, batch, max_pages = 16, 255, 4112
+    n = batch * max_pages
+    full, a, other = (B.KV8Pages(n, page, batch, max_pages) for _ in range(3))
+    full.page_table.copy_(torch.randperm(n, device=DEV).view(batch, max_pages))
+    full.seq_len.fill_(max_pages * page)
+    full.n_free.fill_(0)
+    stay, none = (torch.full((batch,), v, dtype=torch.int32, device=DEV) for v in (-1, 0))
+    cu, pos = torch.zeros(batch + 1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+
+    def time_of(**to):
+        ms = []
+        for _ in range(5):
+            B.sl_kv8_pages_resize(full, stay, cu, pos, 0, to=a)
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            B.sl_kv8_pages_resize(a, none, cu, pos, 0, **to)
+            end.record()
+            torch.cuda.synchronize()
+            ms.append(start.elapsed_time(end))
+        return min(ms)
+
+    beside, in_place = time_of(to=other), time_of()
+    for p in (a, other):
+        assert p.n_free.tolist() == [n] and torch.equal(p.free_pages, full.page_table.view(-1)) and not p.seq_len.any() and (p.page_table == -1).all()
+    assert in_place <= 5 * beside, (in_place, beside)
+
+
+@pytest.mark.parametrize("batch,max_pages,m_upper", [(8, 250, 47), (8, 250, 48), (8, 250, 49), (255, 8, 8), (255, 8, 9), (64, 64, 0), (20, 200, 20)])
+@pytest.mark.parametrize("seed", [1, 2])
+def test_in_place_with_few_rows_and_many_pages(batch, max_pages, m_upper, seed):
+    """Around the size up to which one workgroup does it, and beyond, where lengths are copied first."""
+    rng, page = random.Random(seed), 16
+    lens = [rng.randint(0, max_pages * page) for _ in range(batch)]
+    table, stack, n_free = pool(rng, lens, page, max_pages, batch * max_pages)
+    pages = B.KV8Pages(len(stack), page, batch, max_pages)
+    state(pages, table, lens, stack, n_free)
+    for _ in range(3):
+        want = [rng.choice([-1, 0, 0, n // 2, n + 1, n + rng.randint(0, 5)]) for n in lens]
+        expected = ref.pages_resize(table, lens, stack, n_free, want, page, len(stack), m_upper)
+        check(pages, resize(pages, want, m_upper), expected)
+        table, lens, stack, n_free = expected[:4]
