@@ -601,7 +601,8 @@ int sl_adapters_pack(void *stream, const sl_adapters *ad /* host */, int32_t slo
  *                share one
  * Rows past the count are neither read nor written, and no row touches another's result.  Products are accumulated in fp32; A x[r] is held in
  * fp32 and goes into the second product with 24 bits; a result is rounded once.  A row with an adapter whose x holds a NaN or an infinity,
- * or whose scale A x[r] leaves the range of bf16 (3.4e38), comes out as NaN.  The same sums in the same order in every call of one shape.  m_upper <= 2^16. */
+ * or whose scale A x[r] leaves the range of bf16 (3.4e38), comes out as NaN; an infinity in B gives what it gives in fp32, in its output alone.  The same
+ * sums in the same order in every call of one shape.  m_upper <= 2^16. */
 int sl_adapters_workspace_bytes(const sl_adapters *ad /* host */, int32_t m_upper, size_t *out);
 int sl_adapters_forward(void *stream, const sl_adapters *ad /* host */, const void *x, const int32_t *row_adapter, const int32_t *m_dev,
                         int32_t m_upper, const float *base, int32_t splits, float *y_f32, void *y_bf16, void *workspace,

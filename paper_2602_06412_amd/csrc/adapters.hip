@@ -264,6 +264,26 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(Bank bank, const bf16_
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < CT; ++c) *(f32x4*)&sh[lane & 15][(wave * CT + c) * 16 + (lane >> 4) * 4] = out[c];
+  // An infinity among the weights meets parts of h that are zero, its own or those in the padding: what came out as NaN is summed again with h in one
+  // part.  (Seldom, so all is asked for again; the sum of the results tells whether, without a test of each.)
+  float all = 0.f;
+#pragma unroll
+  for (int c = 0; c < CT; ++c) all += (out[c][0] + out[c][1]) + (out[c][2] + out[c][3]);
+  if (__any(all != all)) {
+#pragma unroll 1
+    for (int i = 0; i < 4 * CT; ++i) {
+      float* result = &sh[lane & 15][wave * CT * 16 + i / 4 * 16 + (lane >> 4) * 4 + i % 4];
+      if (*result == *result) continue;
+      const bf16_t* parts = h + (size_t)rr * bank.rank_tiles * 64;
+      const bf16_t* w = bank.b_of(own) + ((size_t)min(first + i / 4, tiles_n - 1) * mine.tiles * 32 + (lane >> 4) * 4 + i % 4) * 8;
+      float v = 0.f;
+      for (int k = 0; k < mine.tiles * 16; ++k) {
+        const bf16_t* p = parts + k / 16 * 64 + k % 16;
+        v += ((float)p[0] + (float)p[16] + (float)p[32]) * (float)w[k / 8 * 128 + k % 8];
+      }
+      *result = v;
+    }
+  }
   __syncthreads();
   for (int s = 2;; ++s) {
 #pragma unroll

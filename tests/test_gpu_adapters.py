@@ -198,3 +198,27 @@ def test_same_bits_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(ys[0], ys[1]) and torch.equal(ys[0], ys[2])
+
+
+# rows, outputs, largest rank: one, two and four column tiles a wave, and the first product's forms
+@pytest.mark.parametrize("m,n,max_rank", [(6, 33, 16), (40, 72, 40), (260, 4100, 16), (520, 4100, 40), (2050, 1040, 64)])
+@pytest.mark.parametrize("out", [F, BF])
+def test_infinite_weights_of_the_second_product(m, n, max_rank, out):
+    """An infinity in B is one in its output (NaN where two of different signs meet), for the rows of its adapter alone, and leaves other outputs as they are."""
+    ad, weights = bank(3, max_rank, n, 64, {0: max_rank, 1: max(1, max_rank - 3), 2: 1}, 11)
+    a, b, scale = weights[0]
+    hit = b.copy()
+    hit[3, max_rank // 2], hit[n - 1, 0], hit[17, [0, max_rank - 1]], hit[5, 1] = np.inf, -np.inf, [np.inf, -np.inf], np.nan
+    B.sl_adapters_pack(ad, 0, dev(a, BF), dev(hit, BF), scale)
+    which = np.arange(m) % 5 - 1
+    x, base = inputs(m, n, 64, 1, 12)
+    y = forward(ad, x, which, m, m, base, out)
+    mine, cols = np.nonzero(which == 0)[0], [3, n - 1, 17, 5]
+    with np.errstate(invalid="ignore"):
+        want = scale * (f64(x)[mine] @ a.T) @ hit.T[:, cols]
+    assert np.array_equal(f64(y)[mine][:, cols], want, equal_nan=True) and np.isinf(want[:, :2]).all() and np.isnan(want[:, 3]).all()
+    weights[0] = (a, np.where(np.isfinite(hit), hit, 0), scale)
+    y[torch.as_tensor(mine, device=DEV)[:, None], torch.as_tensor(cols, device=DEV)] = 0
+    w, bound = ref.adapters(f64(x), f64(base), list(which), weights)
+    w[np.ix_(mine, cols)] = 0
+    assert (np.abs(f64(y) - w) <= bound + half_step(np.abs(w) + bound, out) * 1.01).all()
