@@ -222,3 +222,32 @@ def test_infinite_weights_of_the_second_product(m, n, max_rank, out):
     w, bound = ref.adapters(f64(x), f64(base), list(which), weights)
     w[np.ix_(mine, cols)] = 0
     assert (np.abs(f64(y) - w) <= bound + half_step(np.abs(w) + bound, out) * 1.01).all()
+
+
+@pytest.mark.parametrize("m,n,k,max_rank", [(5, 40, 64, 16), (33, 100, 520, 40), (260, 4100, 64, 16), (520, 4100, 1032, 40), (1030, 48, 136, 64), (2050, 1040, 64, 64)])
+def test_all_bits_of_the_first_product_reach_the_second(m, n, k, max_rank):
+    """A x is a whole number of 24 bits over 2^16, from three products, and B picks one of its numbers for each output: what comes out may be off by a step of fp32
+    (2^-23) for each of the four sums that are not of zeros.  Sixteen of the 24 bits would not do."""
+    rng = np.random.default_rng(m + n)
+    ad, weights = B.Adapters(3, max_rank, n, k), {}
+    for slot, rank in enumerate((max_rank, max_rank - 1, 7)):
+        a = rng.choice([-1, 1], (rank, k)) * (129 + 2 * rng.integers(0, 64, (rank, k)))
+        b = np.zeros((n, rank))
+        b[np.arange(n), np.arange(n) % rank] = rng.choice([-1, 1, 0.5], n)
+        B.sl_adapters_pack(ad, slot, dev(a, BF), dev(b, BF), 1.0)
+        weights[slot] = (a, b)
+    x = np.zeros((m, k))
+    for r in range(m):
+        x[r, rng.choice(k, 3, replace=False)] = [1, 2.0 ** -8, 2.0 ** -16]
+    which = rng.integers(0, 3, m)
+    y = f64(forward(ad, dev(x, BF), which, m, m, None, F))
+    for slot, (a, b) in weights.items():
+        rows = which == slot
+        if not rows.any():
+            continue
+        h = x[rows] @ a.T
+        want = h @ b.T
+        assert (np.abs(y[rows] - want) <= np.abs(want) * 2.0 ** -21).all()
+        high = f64(torch.tensor(h).to(BF))
+        cut = (high + f64(torch.tensor(h - high).to(BF))) @ b.T
+        assert (np.abs(cut - want) > np.abs(want) * 2.0 ** -21).mean() > 0.5
