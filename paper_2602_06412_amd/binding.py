@@ -668,11 +668,13 @@ def sl_adapters_pack(ad, slot, a, b, scale=1.0):
     """a [rank, k], b [n, rank] (bfloat16); None for both empties the slot."""
     dev, stream = _adapters_here(ad)
     rank = 0
+    if (a is None) != (b is None):
+        raise ValueError("a and b are needed together, or neither")
     if a is not None:
         rank = a.shape[0]
         if tuple(a.shape) != (rank, ad.k) or tuple(b.shape) != (ad.n, rank):
             raise ValueError(f"a [rank, {ad.k}] and b [{ad.n}, rank] are needed, not {tuple(a.shape)} and {tuple(b.shape)}")
-    _check("sl_adapters_pack", lib().sl_adapters_pack(stream, ad.desc_ref, slot, rank, scale, _addr(a, _BF16, dev), None if a is None else _addr(b, _BF16, dev)))
+    _check("sl_adapters_pack", lib().sl_adapters_pack(stream, ad.desc_ref, slot, rank, scale, _addr(a, _BF16, dev), _addr(b, _BF16, dev)))
 
 
 def sl_adapters_workspace_bytes(ad, m_upper):

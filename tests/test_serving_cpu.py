@@ -271,3 +271,12 @@ def test_turns_by_hand():
     assert np.allclose(f * 2 * np.pi, [1.0, 0.1])
     assert np.allclose(ref.rope_freqs(4, 100.0, "linear", 4.0), f / 4) and np.allclose(ref.rope_freqs(4, 100.0, "base", 4.0) * 2 * np.pi, [1.0, 1600 ** -0.5])
     assert np.allclose(ref.rope_freqs(4, 100.0, "turns", 4.0, 2 * np.pi * 10, 1.0, 10.0), [f[0], f[1] / 4])
+
+
+@pytest.mark.parametrize("change", [dict(a=None), dict(b=None)])
+def test_half_an_adapter_is_refused(library, change):
+    with pytest.raises(ValueError):
+        B.sl_adapters_pack(**dict(pack(), **change))
+    assert library.calls == []
+    B.sl_adapters_pack(**dict(pack(), a=None, b=None))            # (empties the slot)
+    assert library.calls == ["sl_adapters_pack"]
