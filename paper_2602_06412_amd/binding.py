@@ -624,6 +624,8 @@ def sl_rope_rows(q, q_out, k, k_out, freqs, row_pos, m_dev, m_upper, interleaved
     kp = ks = ko = kos = None
     kv_heads = 0
     if k is not None:
+        if k_out is None:
+            raise ValueError("keys need a k_out")
         kv_heads = k.shape[1]
         (kp, ks), (ko, kos) = _head_rows(k, t_in, dev, kv_heads, d, m_upper), _head_rows(k_out, t_out, dev, kv_heads, d, m_upper)
     status = lib().sl_rope_rows(stream, qp, qs, qo, qos, heads, kp, ks or 0, ko, kos or 0, kv_heads, _float_code(q), _float_code(q_out), d, 2 * freqs.numel(),

@@ -280,3 +280,12 @@ def test_half_an_adapter_is_refused(library, change):
     assert library.calls == []
     B.sl_adapters_pack(**dict(pack(), a=None, b=None))            # (empties the slot)
     assert library.calls == ["sl_adapters_pack"]
+
+
+def test_keys_without_a_place_for_them_are_refused(library):
+    with pytest.raises(ValueError):
+        B.sl_rope_rows(**dict(rope(), k_out=None))
+    assert library.calls == []
+    B.sl_rope_rows(**dict(rope(), k=None, k_out=None))
+    B.sl_rope_rows(**dict(rope(), k=None))                        # (k_out is not looked at)
+    assert library.calls == ["sl_rope_rows"] * 2
