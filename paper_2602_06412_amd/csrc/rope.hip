@@ -151,9 +151,10 @@ int slk_rope_rows(hipStream_t s, const void* q, int64_t q_stride, void* q_out, i
                   float amplitude, const int32_t* row_pos, const int32_t* m_dev, int m_upper) {
   const RopeArgs a{{{q, q_out, q_stride, q_out_stride, n_heads}, {k, k_out, k_stride, k_out_stride, k ? n_kv_heads : 0}},
                    freqs, row_pos, m_dev, m_upper, d, rot, amplitude};
-  // numbers at a time: eight of bf16, four where one side is fp32, if every piece of them is aligned.  40 heads of 128 bf16, replayed, 8 / 4 / 1 at
-  // a time: 512 rows 3.8 / 4.0 / 5.2 us, 8192 rows 26.0 / 26.0 / 31.1; 5533 rows of 64 heads 36 us of eight, 49 of one
-  const int most = dtype_in == SL_BF16 && dtype_out == SL_BF16 ? 8 : 4;
+  // numbers at a time: eight of bf16 where pairs lie apart, else four, if every piece of them is aligned.  40 heads of 128 bf16, replayed, 8 / 4 / 1 at a
+  // time, us: apart 64 rows 3.2 / 3.4 / 4.4, 512 rows 4.0 / 4.2 / 5.4, 2048 rows 7.9 / 8.3 / 11.1, 8192 rows 26.0 / 26.0 / 30.7; interleaved
+  // 512 rows 4.3 / 4.1 / 5.3, 2048 rows 9.1 / 7.7 / 10.3, 8192 rows 26.8 / 25.9 / 29.8.
+  const int most = dtype_in == SL_BF16 && dtype_out == SL_BF16 && !pairs ? 8 : 4;
   auto fits = [&](int v) {
     auto side = [&](const RopeSide& x) {
       return ((uintptr_t)x.in % (v * sl_tsize(dtype_in)) | (uintptr_t)x.out % (v * sl_tsize(dtype_out))) == 0 && x.in_stride % v == 0 && x.out_stride % v == 0;
@@ -172,7 +173,7 @@ int slk_rope_rows(hipStream_t s, const void* q, int64_t q_stride, void* q_out, i
   } while (0)
   if (dtype_in == SL_BF16) {
     if (dtype_out == SL_BF16) {
-      if (v == 8) ROPE_BY_LAYOUT(bf16_t, bf16_t, 8); else ROPE_RUN(bf16_t, bf16_t);
+      if (v == 8) ROPE_LAUNCH(bf16_t, bf16_t, false, 8); else ROPE_RUN(bf16_t, bf16_t);
     } else {
       ROPE_RUN(bf16_t, float);
     }
