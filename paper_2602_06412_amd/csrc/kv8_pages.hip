@@ -238,11 +238,14 @@ int slk_kv8_pages_resize(hipStream_t s, const sl_kv8_pages* from, const sl_kv8_p
   a.m_upper = m_upper;
   a.seq_len = from->seq_len;
   a.n_free = from->n_free;
-  // In place, what a step writes is bounded by its rows and the pages that it may give up, which are as many as there are however few the rows.  Up to
-  // 2048 of both one workgroup does it, without the copy below.  One / by the rule for many, replayed, us: 8 sequences of 32 pages 3.1 / 4.5;
-  // 32 of 32, a slot more each 4.3 / 5.0, all end 5.1 / 4.7; 64 of 64 5.8 / 5.4 and 11.8 / 5.0; 255 of 64 15.8 / 5.3 and 38.7 / 5.0; 255 of 4112, all end 2395 / 9.3.
-  const int64_t entries = (int64_t)a.batch * a.max_pages, numbers = m_upper + (a.apart ? entries + a.n_pages : min(entries, (int64_t)a.n_pages));
-  const unsigned grid = !a.apart && numbers <= 2048 ? 1 : grid_for(numbers);
+  // In place a step may give up all pages that there are, however few its rows.  One workgroup does it without the copy below, if its lanes go few times
+  // over the pieces of new rows and over those pages.  One / many workgroups, replayed, us, where every sequence takes a slot, and where all end: 8
+  // sequences of 32 pages 3.1 / 4.6 and 3.0 / 4.5, 32 of 32 4.1 / 5.1 and 4.8 / 4.9, 64 of 64 5.7 / 5.1 and 11.5 / 4.9, 255 of 64 15.7 / 5.4 and 38.7 / 5.0,
+  // 64 of 1024 5.8 / 5.2 and 148 / 5.0, 255 of 4112 15 / 5.2 and 2392 / 9.2.
+  const int64_t entries = (int64_t)a.batch * a.max_pages, gives = min(entries, (int64_t)a.n_pages);
+  const int64_t pieces = min((int64_t)m_upper, 2 * (int64_t)a.batch + m_upper / from->page_slots);
+  const bool one = !a.apart && pieces * min(from->page_slots, 64) <= 2048 && gives <= 8192;
+  const unsigned grid = one ? 1 : grid_for(m_upper + (a.apart ? entries + a.n_pages : gives));
   if (!a.apart && grid > 1) {
     // in place: the first workgroup writes lengths that others may not have read yet, so all read a copy
     hipLaunchKernelGGL(kv8_pages_lengths_kernel, dim3(1), dim3(kThreads), 0, s, from->seq_len, from->n_free, a.batch, (int32_t*)workspace);

@@ -185,7 +185,7 @@ def test_many_pages_given_up_in_place_take_no_longer_than_beside():
     assert in_place <= 5 * beside, (in_place, beside)
 
 
-@pytest.mark.parametrize("batch,max_pages,m_upper", [(8, 250, 47), (8, 250, 48), (8, 250, 49), (255, 8, 8), (255, 8, 9), (64, 64, 0), (20, 200, 20)])
+@pytest.mark.parametrize("batch,max_pages,m_upper", [(8, 250, 47), (64, 128, 128), (64, 128, 129), (32, 256, 32), (33, 249, 33), (255, 8, 8), (64, 64, 0), (20, 600, 20)])
 @pytest.mark.parametrize("seed", [1, 2])
 def test_in_place_with_few_rows_and_many_pages(batch, max_pages, m_upper, seed):
     """Around the size up to which one workgroup does it, and beyond, where lengths are copied first."""
