@@ -207,9 +207,11 @@ __global__ __launch_bounds__(kThreads) void kv8_pages_init_kernel(Pages to, int 
   if (start == 0) *to.n_free = n_pages;
 }
 
-// One number a thread: workgroups that take 2048 each are too few (255 sequences that decode 10.3 us, 512 each 7.1, 256 each 6.2; of as
-// few as 128 nothing is gained).  More than 512 workgroups form the sums oftener than they save (2048 of them: 16.9 us for 15.7).
-unsigned grid_for(int64_t numbers) { return (unsigned)max((int64_t)1, min((int64_t)512, (numbers + 255) / 256)); }
+// One number a thread, and at most 1024 workgroups, each of which forms the sums.  Replayed, us: numbers a workgroup 2048 / 512 / 256 / 128,
+// 255 sequences that decode 9.4 / 6.2 / 5.4 / 5.4; workgroups at most 512 / 1024 / 2048, 64 sequences with prompts 7.7 / 6.6 / 6.6, 255 sequences of as many
+// as 4096 pages that decode 9.5 / 8.6 / 8.5, 255 with prompts in pages of 64 11.3 / 9.2 / 8.5, in pages of 16 6.2 / 6.3 / 6.6, 255 of 4112 pages that all end, in
+// place, 9.2 / 7.7 / 8.0.
+unsigned grid_for(int64_t numbers) { return (unsigned)max((int64_t)1, min((int64_t)1024, (numbers + 255) / 256)); }
 
 }  // namespace
 
@@ -241,7 +243,7 @@ int slk_kv8_pages_resize(hipStream_t s, const sl_kv8_pages* from, const sl_kv8_p
   // In place a step may give up all pages that there are, however few its rows.  One workgroup does it without the copy below, if its lanes go few times
   // over the pieces of new rows and over those pages.  One / many workgroups, replayed, us, where every sequence takes a slot, and where all end: 8
   // sequences of 32 pages 3.1 / 4.6 and 3.0 / 4.5, 32 of 32 4.1 / 5.1 and 4.8 / 4.9, 64 of 64 5.7 / 5.1 and 11.5 / 4.9, 255 of 64 15.7 / 5.4 and 38.7 / 5.0,
-  // 64 of 1024 5.8 / 5.2 and 148 / 5.0, 255 of 4112 15 / 5.2 and 2392 / 9.2.
+  // 64 of 1024 5.8 / 5.2 and 148 / 5.0, 255 of 4112 15 / 5.2 and 2392 / 7.6.
   const int64_t entries = (int64_t)a.batch * a.max_pages, gives = min(entries, (int64_t)a.n_pages);
   const int64_t pieces = min((int64_t)m_upper, 2 * (int64_t)a.batch + m_upper / from->page_slots);
   const bool one = !a.apart && pieces * min(from->page_slots, 64) <= 2048 && gives <= 8192;
