@@ -944,9 +944,12 @@ extern "C" int sl_adapters_forward(void* stream, const sl_adapters* ad, const vo
 }
 
 // ---- draws from a filtered posterior -----------------------------------------------------------------------
+// The workspace is part of the call only: all sums stay on the CU, and no kernel gets its address.
+static constexpr size_t kSampleWorkspace = 256;
+
 extern "C" int sl_sample_filtered_bytes(int32_t m_upper, int32_t vocab, size_t* out) {
   if (!out || m_upper < 0 || m_upper > 1 << 20 || vocab < 1 || vocab > 1 << 18) return SL_EINVAL;
-  *out = slk_sample_filtered_bytes(m_upper, vocab);
+  *out = kSampleWorkspace;
   return SL_OK;
 }
 
@@ -961,7 +964,7 @@ extern "C" int sl_sample_filtered(void* stream, const void* logits, int32_t dtyp
        (uintptr_t)token | (uintptr_t)prob | (uintptr_t)kept) % 4) return SL_EINVAL;
   if (!workspace || (uintptr_t)workspace % 256) return SL_EINVAL;
   if (m_upper == 0) return SL_OK;
-  if (workspace_bytes < slk_sample_filtered_bytes(m_upper, vocab)) return SL_ENOSPC;
+  if (workspace_bytes < kSampleWorkspace) return SL_ENOSPC;
   return slk_sample_filtered((hipStream_t)stream, logits, dtype, row_stride, n_rows, vocab, row_map, m_dev, m_upper, temperature, top_k, top_p, min_p,
-                             uniform, token, prob, kept, workspace);
+                             uniform, token, prob, kept);
 }

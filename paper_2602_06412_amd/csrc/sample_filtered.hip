@@ -724,11 +724,9 @@ __global__ __launch_bounds__(NT, 4) void sample_filtered_kernel(SampleArgs a) {
 
 }  // namespace
 
-size_t slk_sample_filtered_bytes(int m_upper, int vocab) { return 256; }
-
 int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t row_stride, int n_rows, int vocab, const int32_t* row_map,
                         const int32_t* m_dev, int m_upper, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-                        const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace) {
+                        const float* uniform, int32_t* token, float* prob, int32_t* kept) {
   const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
 #define SAMPLE_RUN(T, NT) hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), 0, s, a)
   // Rows beyond the CUs: two workgroups of 512 threads a CU pass over more rows at a time, one of 1024 over a row faster.  512 / 1024 threads,

@@ -419,10 +419,9 @@ size_t slk_adapters_workspace_bytes(const sl_adapters* ad, int m_upper);
 int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, const int32_t* row_adapter, const int32_t* m_dev, int m_upper,
                          const float* base, int splits, float* y_f32, void* y_bf16, void* workspace);
 // sample_filtered.hip: draws from a filtered posterior
-size_t slk_sample_filtered_bytes(int m_upper, int vocab);
 int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t row_stride, int n_rows, int vocab, const int32_t* row_map,
                         const int32_t* m_dev, int m_upper, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
-                        const float* uniform, int32_t* token, float* prob, int32_t* kept, void* workspace);
+                        const float* uniform, int32_t* token, float* prob, int32_t* kept);
 // attention_mfma.hip
 int slk_attention_mfma(hipStream_t s, const void* q, const void* kc, const void* vc, const int32_t* active_idx,
                        const int32_t* m_dev, int m_upper, int B, int H, int N, int n_pad, void* o, float* scratch);
