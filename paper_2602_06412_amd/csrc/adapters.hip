@@ -15,7 +15,7 @@
 //
 // What bounds it: waiting for one load after another (a row's adapter, its rank, h, weights), twice.  One row of 4096, 7.8 us replayed, two
 // launches of 4; 64 rows of 64 adapters of rank 16, 4096 to 12288 beside fp32, 17.3 us (8.3 and 9.8 for 31 MB in all, at the rate of a large read 4.5);
-// 1100 rows in runs of one adapter of rank 64, 12288 to 4096 beside two partial sums, 36 us (20.3 and 16 for 83 MB, at that rate 12.2).
+// 1100 rows in runs of one adapter of rank 64, 12288 to 4096 beside two partial sums, 36 us (20.1 and 16.5 for 83 MB, at that rate 12.2).
 #include "sl_common.h"
 
 namespace {
@@ -344,10 +344,11 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
                          const float* base, int splits, float* y_f32, void* y_bf16, void* workspace) {
   const Bank bank = bank_of(ad);
   bf16_t* h = (bf16_t*)workspace;
-  // Rank tiles a workgroup: as many as leave a workgroup for every second CU (each reads the rows again).  1100 rows of rank 64, the whole call with
-  // 1 / 2 / 4 tiles: 52.3 / 43.5 / 46.9 us.  Adapters of sixteen rows side by side: all of them while that is no more than four workgroups a
-  // CU, and two at least.  One / by this rule / sixteen: 16 rows of 16 adapters 52 / 13.1 / 13.1 us, 512 rows of 64 63 / 23.8 / 23.9, 2048 rows
-  // of 64 90 / 62.4 / 68.3, 2048 rows in runs of 200 23.5 / 21.3 / 24.4.
+  // Rank tiles a workgroup: as many as leave a workgroup for every second CU (each reads the rows again).  The whole call with 1 / 2 / 4 tiles, us: 1100
+  // rows of rank 64 and 12288 inputs 45.4 / 37.2 / 40.8, 2048 rows of rank 64 and 4096 33.6 / 34.3 / 32.4, 512 rows of rank 64 17.5 / 17.6 / 18.4, 64 rows of
+  // rank 64 23.3 / 24.8 / 27.6.  Adapters of sixteen rows side by side: all of them while that is no more than four workgroups a
+  // CU, and two at least.  One / by this rule / sixteen: 16 rows of 16 adapters 52 / 13.1 / 13.2 us, 512 rows of 64 63 / 23.4 / 23.7, 2048 rows
+  // of 64 93 / 65 / 71, 2048 rows in runs of 200 25.3 / 22.2 / 26.3.
   const int tiles = bank.rank_tiles, groups = sl_cdiv(m_upper, kRows);
 #define DOWN_RUN(RT, P)                                                                                                            \
   do {                                                                                                                             \
@@ -364,8 +365,9 @@ int slk_adapters_forward(hipStream_t s, const sl_adapters* ad, const void* x, co
 #undef DOWN_RUN
   SL_LAUNCH_CHECK();
   // Column tiles a wave: more of them share the reading of h and of the rows' adapters, once there are waves enough.  The whole call with 1 / 2 /
-  // 4: 64 rows by 4096 of rank 64 (1024 waves of one tile) 27.2 / 33.3 / - us, 64 rows by 12288 (3,000) 23.6 / 21.0 / 21.4, 256 rows by 12288
-  // (12,000) - / 18.8 / 16.5, 2048 rows by 4096 (33,000) - / 25.8 / 24.7.
+  // 4, us, adapters of rank 16 at random: 64 rows by 4096 (1024 waves of one tile) 13.9 / 14.6 / 17.6, 64 by 8192 (2048) 15.1 / 15.3 / 18.0, 64 by 12288 (3,000)
+  // 17.1 / 17.2 / 19.2, 128 by 8192 (4096) 18.3 / 17.6 / 19.1, 128 by 12288 (6,000) 21.4 / 20.3 / 20.8, 256 by 8192 (8192) 24.8 / 23.9 / 21.8, 256 by 12288
+  // (12,000) 29.6 / 27.9 / 24.4, 2048 by 4096 (33,000) 76.7 / 73.1 / 65.4; of rank 64, 64 by 12288 28.9 / 30.5 / 39.0, 128 by 12288 in runs 15.3 / 14.4 / 14.8.
 #define UP_RUN(T, CT, D, Y)                                                                                                         \
   hipLaunchKernelGGL((adapters_up_kernel<T, CT, D>), dim3(sl_cdiv(sl_cdiv(ad->n, 16), 4 * CT), groups), dim3(256),    \
                      max(kRows * (tiles * 8 + 1) * 16, kRows * (64 * CT + 4) * 4), s, bank, h, row_adapter, m_dev, m_upper, base, splits, Y)

@@ -9,8 +9,9 @@
 //   returns    a page given up and not taken: onto the stack, and its entry cleared
 //   copies     (states apart) all other entries of the table and of the stack
 // Every workgroup forms the prefix sums again from the lengths, a wave for all 255 sequences, lanes moved instead of LDS: no second launch, no
-// atomics.  What bounds it is the chain of loads and sums of that wave and one search in them, not bytes.  Replayed from a graph: 3 sequences
-// 4.2 us (3 us are a launch's own), 255 sequences that decode 5.4 us, 64 sequences of which half want 176000 slots more, not all of which fit, 7.6 us.
+// atomics.  What bounds it is the chain of loads and sums of that wave and one search in them, not bytes.  Replayed from a graph, into another state: 3
+// sequences 4.3 us (3 us are a launch's own), 255 sequences that decode 5.4 us, 64 sequences of which half want 176000 slots more, not all of which fit, 6.6 us.
+// In place: 8 sequences that decode 3.1 us, 255 sequences 5.3 us, of which 1.5 are the copy of the lengths that goes before.
 #include "sl_common.h"
 
 namespace {

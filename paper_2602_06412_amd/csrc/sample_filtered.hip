@@ -7,20 +7,23 @@
 // A workgroup takes a row and passes over it as often as it has to, 32 to 64 bytes a thread in flight.  Of bf16 that is twice (counts, with the
 // largest number; then weights in order of ids), and what bounds it is those reads and an LDS access a token: 1024 rows of 126464, top-p and min-p, 113 us,
 // 4.6 TB/s over both passes (one read of all rows at the rate of a large one: 38 us); 64 rows, top-k and top-p, 36 us, each
-// on a CU of its own, whose share of the passes is 11 GB/s times 1000 and the rest the search for two borders.  Several workgroups a row, in three launches, were slower
-// for top-k (27 -> 30 us), for many rows and for short ones, and gained a tenth in the best case: one workgroup it is.
+// on a CU of its own: 506 KB in two passes, at 14 GB/s with the searches for two borders among them (1 row: top-p 36 us, top-k 26).  Several workgroups a row, in three
+// launches, gained where there is no filter (64 rows 28 -> 21 us, 1 row 26 -> 18) and a tenth with top-p, but were slower for top-k (27 -> 30), for many rows and
+// for short ones: one workgroup it is.
 //
 // Weights.  2^t = 2^n T[i] 2^(r / 256) with 256 t = 256 n + i + r, |r| <= 1 / 2: a table of 256 powers and a sum of four terms, off by
 // less than 2^-51 of itself.
 // bf16.  A weight depends on 16 bits, and logits take a few thousand of the 65536 numbers.  These are counted one by one (LDS, an atomic
 // add of one a token): order, sums of weights and borders follow from counts times weights, and the exponential is
 // taken once for each number that occurs; the last pass reads the weights of what is kept from a table.  Numbers below 2^-10 in size, nearly
-// half of the 65536 and hardly any logit, share one bin and are weighed token by token.
+// half of the 65536 and hardly any logit, share one bin and are weighed token by token.  The pass also finds the largest number if that is positive and not tiny; rows of
+// log-probabilities are passed over once more for it (64 rows, top-p 36 -> 38 us, top-k 28 -> 37; 1024 rows 114 -> 136 and 90 -> 135).  Numbers that are all tiny, or all
+// alike, meet in one place of LDS, token by token: a row of 126464 zeros takes 530 us with top-p, 1024 of them 1950 (no filter 62 and 228).
 // fp32, and bf16 where that does not do (a border among the tiny numbers, a temperature in the hundreds): the border's key in three
 // steps of 11, 11 and 10 bits that add up weights (or counts) for each value of the digit.  The first is a pass over the row; the second lists the
 // keys that begin with the first's digit, in LDS, and it and the third work on the list (if that has no room for all, on the row).  What bounds
-// it is the fp64 of a weight for each token and pass: 64 rows of 126464 fp32, top-p, 116 us (130 with three passes over the row),
-// top-k 63 (76; 68 with a pass of its own for the first digit), no filter 49.
+// it is the fp64 of a weight for each token and pass: 64 rows of 126464 fp32, top-p, 116 to 121 us (130 with three passes over the row),
+// top-k 63 to 65 (76; 68 with a pass of its own for the first digit), both 92, no filter 50; 1 row 115, 61, 87 and 47.
 #include "sl_common.h"
 
 namespace {
@@ -730,10 +733,10 @@ int slk_sample_filtered(hipStream_t s, const void* logits, int dtype, int64_t ro
   const SampleArgs a{logits, row_stride, n_rows, vocab, m_upper, row_map, m_dev, top_k, temperature, top_p, min_p, uniform, token, prob, kept};
 #define SAMPLE_RUN(T, NT) hipLaunchKernelGGL((sample_filtered_kernel<T, NT>), dim3(m_upper), dim3(NT), 0, s, a)
   // Rows beyond the CUs: two workgroups of 512 threads a CU pass over more rows at a time, one of 1024 over a row faster.  512 / 1024 threads,
-  // us: 126464 bf16 64 rows 40.4 / 36.4, 256 rows 46.2 / 41.8, 300 rows 59 / 64, 512 rows 64 / 78, 1024 rows 117 / 148; 8192 bf16 256 rows
-  // 12.6 / 13.7, 512 rows 16 / 24; 126464 fp32 256 rows 187 / 150, 300 rows 231 / 176, 384 rows 237 / 235, 512 rows 246 / 251; 8192 fp32
-  // 300 rows 24.9 / 25.3, 384 rows 25 / 33.  And few rows that are short, of which most is waiting for one another: 3 rows of 1024 bf16 9.6 / 10.7,
-  // 8192 bf16 12.0 / 13.0, 16384 bf16 14.3 / 14.7, 1024 fp32 10.6 / 11.8, 4096 fp32 14.8 / 15.1, 8192 fp32 19.6 / 18.3 (256 threads are slower than 512).
+  // us, top-p: 126464 bf16 64 rows 40.6 / 36.3, 256 rows 46.5 / 41.9, 300 rows 59 / 65, 512 rows 63 / 78, 1024 rows 117 / 145; 8192 bf16 256 rows
+  // 12.4 / 13.4, 512 rows 16 / 24; 126464 fp32 256 rows 175 / 135, 300 rows 230 / 179, 384 rows 236 / 239, 512 rows 247 / 254; 8192 fp32
+  // 300 rows 25.1 / 25.7, 384 rows 25 / 34.  And few rows that are short, of which most is waiting for one another: 3 rows of 1024 bf16 9.6 / 11.0,
+  // 8192 bf16 12.0 / 13.0, 16384 bf16 14.3 / 14.8, 1024 fp32 11.2 / 12.8, 4096 fp32 15.0 / 15.7, 8192 fp32 19.7 / 18.8 (256 threads are slower than 512).
   const bool many = m_upper > (dtype == SL_BF16 ? 256 : 320) || vocab * sl_tsize(dtype) <= 16384;
   if (dtype == SL_BF16) {
     if (many) SAMPLE_RUN(bf16_t, 512); else SAMPLE_RUN(bf16_t, 1024);
